@@ -107,18 +107,19 @@ def _page_size(case):
 
 # ---------------------------------------------------------------------------------------------------------- the 4-bit rows
 def _quantize(x):
-    """Codes 0..15 (uint8), step and zero-point (float32) of the rows of x (float32)."""
+    """Codes 0..15 (uint8), step and zero-point (float32) of the rows of x, in 64 bits: 16-bit values often lie on a border."""
+    x = x.double()
     lo, hi = x.amin(-1).clamp(max=0.0), x.amax(-1).clamp(min=0.0)
-    step = (hi - lo) / 13.0
-    step = ((step.view(torch.int32) + 8) & -16).view(torch.float32)
+    step = (((hi - lo) / 13.0).view(torch.int64) + (1 << 32)) & -(1 << 33)
+    step = step.view(torch.float64)
     live = step >= F32_MIN
-    inv = torch.where(live, 1.0 / step, 0.0)
-    zero = torch.round(-lo * inv).clamp(0.0, 13.0)
-    u = x * inv[..., None]
+    step = torch.where(live, step, math.inf)
+    zero = torch.round(-lo / step).clamp(0.0, 13.0)
+    u = x / step[..., None]
     code = (torch.round(u) + zero[..., None]).clamp(0.0, 13.0).to(torch.uint8)
     code = torch.where((u > 0.25) & (u <= 0.75), 14, code)
     code = torch.where((u < -0.25) & (u >= -0.75), 15, code)
-    return code.to(torch.uint8), torch.where(live, step, 0.0), zero
+    return code.to(torch.uint8), torch.where(live, step, 0.0).float(), zero.float()
 
 
 def _pack(code):
@@ -197,7 +198,7 @@ def prepare(case, seed):
         return st
     cache = []
     for gain in (1.0, 0.5):
-        code, step, zero = _quantize(_cached(g, B, H, each * P, D, gain).to(dt).float())
+        code, step, zero = _quantize(_cached(g, B, H, each * P, D, gain).to(dt))
         packed, words = _pack(code), _words(step, zero)
         for x in (packed, words):
             x = x.reshape(B, H, each, P, -1).transpose(1, 2).reshape(pages, H, P, -1)
@@ -217,12 +218,13 @@ def run(st):
 
 
 def _run_norm(st):
-    """The int8 activations as the values they stand for, their scales, and the sum that the next layer adds to."""
+    """The int8 activations as the values they stand for (in the activations' type), their scales, and the sum that the next layer adds to."""
     x, r, w, s = st["x"], st["r"], st["w"], st["s"]
     if own:
         import paper_2311_05161_amd as lib
         q, sx, h = lib.rms_norm_act_int8(x, w, eps=st["eps"], residual=r, s=s)
-        return (q * sx[:, None], sx, h) if r is not None else (q * sx[:, None], sx)
+        y = torch.mul(q, sx[:, None], out=torch.empty_like(x))
+        return (y, sx, h) if r is not None else (y, sx)
     h = x if r is None else (x.float() + r.float()).to(x.dtype)
     f = h.float()
     gain = w.float() if s is None else w.float() * (1.0 / s)
@@ -233,7 +235,8 @@ def _run_norm(st):
     live = torch.isfinite(inv)
     sx = torch.where(live, (a * norm / 127.0).float(), 1.0)
     q = torch.round(u * torch.where(live, inv, 0.0)[:, None]).clamp(-127.0, 127.0)
-    return (q * sx[:, None], sx, h) if r is not None else (q * sx[:, None], sx)
+    y = (q * sx[:, None]).to(x.dtype)
+    return (y, sx, h) if r is not None else (y, sx)
 
 
 def _run_cache(st):
@@ -248,7 +251,7 @@ def _run_cache(st):
     there = torch.arange(S, device=k.device) < st["count"][:, None]
     to, at = page[there], place[there]
     for x, packed, words in ((k, *st["cache"][:2]), (v, *st["cache"][2:])):
-        code, step, zero = _quantize(x.float())
+        code, step, zero = _quantize(x)
         packed[to, :, at] = _pack(code)[there]
         words[to, :, at] = _words(step, zero)[there]
     return tuple((_unpack(packed[page, :, place], words[page, :, place]) * there[:, :, None, None]).to(k.dtype)
@@ -294,13 +297,18 @@ def work(case):
 LEVELS = [2 * c for c in range(0, 14, 2)] + [None] + [2 * c for c in range(1, 14, 2)] + [None]     # of nibbles 0..15, in half steps
 
 
+def _pow2(e):
+    """2 ** e exactly (a library's power may be off in its last bit), normal range."""
+    return (e.to(torch.int64) + 1023 << 52).view(torch.float64)
+
+
 def _values64(packed, words):
     """The rows' values in float64, from the nibbles' levels."""
     lut = torch.tensor([x or 0 for x in LEVELS], dtype=torch.float64, device=packed.device)
     out = torch.empty((*packed.shape[:-1], 2 * packed.shape[-1]), dtype=torch.float64, device=packed.device)
     w = words.to(torch.int64) & 0xFFFFFFFF
     zero, bits = w % 16, w // 16 * 16
-    step = torch.where(bits > 0, torch.ldexp(1.0 + (bits % 8388608).double() / 8388608, bits // 8388608 - 127), 0.0)
+    step = torch.where(bits > 0, (1.0 + (bits % 8388608).double() / 8388608) * _pow2(bits // 8388608 - 127), 0.0)
     for byte in range(packed.shape[-1]):
         for shift, channel in ((1, byte // 4 * 8 + byte % 4), (16, byte // 4 * 8 + byte % 4 + 4)):
             e = packed[..., byte].to(torch.int64) // shift % 16
@@ -324,7 +332,7 @@ def exact(case, seed):
         for x in (st["k"].double(), st["v"].double()):
             low, high = x.min(-1, keepdim=True).values.clamp(max=0), x.max(-1, keepdim=True).values.clamp(min=0)
             frac, power = torch.frexp((high - low) / 13)
-            step = torch.ldexp(torch.floor(frac * 2.0 ** 20 + 0.5), power - 20)      # 20 bits, halves up
+            step = torch.floor(frac * 2.0 ** 20 + 0.5) * _pow2(power - 20)      # 20 bits, halves up
             z = torch.round(-low / step)
             u = x / step
             level = torch.minimum(torch.maximum(torch.round(u), -z), 13 - z)
