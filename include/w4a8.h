@@ -386,6 +386,76 @@ int dint_error_terms(const void *X, int x_dtype, int64_t M, int64_t K, int64_t l
                      int w_dtype, int64_t N, int64_t ldw, const float *s, int64_t group_size, int format,
                      double *terms, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Around the layer in a decoder: the norm in front of it, the 4-bit cache of Keys and Values, attention over that cache. ---- */
+
+/* Root-mean-square norm straight to the layer's int8 activations, with the residual's addition:
+ *     h = cast(X + R)      (R == NULL: h = X);     t[m,k] = h[m,k] * (w[k] * (1 / s[k]))     (s == NULL: h * w);
+ *     a[m] = max_k |t[m,k]|;     Xq[m,k] = rne(t[m,k] * (127 / a[m]));     sx[m] = a[m] / sqrt(mean_k h[m,k]^2 + eps) / 127
+ * i.e. quantize_act_int8 of the normalized row: the norm's factor is the same for the whole row and only reaches sx.  Steps up
+ * to Xq are IEEE binary32 operations as in quantize_act_int8 (a row whose 127 / a is not finite gives sx = 1, Xq = 0); the
+ * mean and sx are evaluated in binary64 and sx is rounded once.
+ *   X    in   [M, ldx], R  in  [M, ldr] or NULL, both of x_dtype (F32, F16 or BF16)
+ *   w    in   [K] of w_dtype: x_dtype or F32           s    in   [K] float or NULL (the AQAS scale)
+ *   H    out  [M, ldh] of x_dtype, the sum for the next residual; may lie on X or R (same rows); only with R
+ *   Xq   out  [M, K] int8, contiguous                  sx   out  [M] float
+ * K >= 1, M == 0 is a no-op. */
+int rms_norm_act_int8(const void *X, int x_dtype, int64_t M, int64_t K, int64_t ldx, const void *R, int64_t ldr, const void *w,
+                      int w_dtype, double eps, const float *s, void *H, int64_t ldh, int8_t *Xq, float *sx, void *stream);
+
+/* The 4-bit cache of Keys and Values, in pages.  A row is one (token, head): head_dim channels in the code space of
+ * quantize_weight_dint4 with the row for the group,
+ *     lo = min(0, min x), hi = max(0, max x);   step = (hi - lo) / 13, rounded to 20 significant bits (half up);
+ *     z = rne(-lo / step);   u = x / step:  1/4 < u <= 3/4 -> +step/2;  -3/4 <= u < -1/4 -> -step/2;
+ *     else step * (clamp(rne(u) + z, 0, 13) - z);        step below the smallest normal number: all zeros, step 0
+ * (F16 and BF16 rows: as in exact arithmetic, ties and borders included).  Its head_dim / 2 bytes are the tiled layout's words
+ * in a row (word q: channels 8q .. 8q+7, see W4A8_LAYOUT_TILED), its word the bits of the step with z in the last four.
+ *   k_packed, v_packed   [pages, heads, page_size, head_dim / 2] bytes      k_words, v_words   [pages, heads, page_size] int32
+ * All four 16-byte aligned; head_dim a multiple of 8, 8 .. 512; page_size >= 1.
+ * (The struct is read on the host; its pointers are device pointers.) */
+typedef struct {
+    uint8_t *k_packed;
+    int32_t *k_words;
+    uint8_t *v_packed;
+    int32_t *v_words;
+    int64_t pages, heads, page_size, head_dim;
+} w4a8_kv_cache;
+
+/* Where the tokens of one step are.  Sequence b has start[b] cached tokens before the step and count[b] <= new_tokens new ones
+ * (count == NULL: new_tokens each), at positions start[b], start[b] + 1, ..; position p lies in page
+ * table[b * table_ld + p / page_size] at place p % page_size.  The arrays are device memory that no call can check before its
+ * launch: a negative or too large start or count is clamped to the table, and a position whose page is not one of the cache's is
+ * neither written nor seen.  table_pages * page_size < 2^31. */
+typedef struct {
+    const int32_t *start;   /* [batch]                                 */
+    const int32_t *count;   /* [batch] or NULL                         */
+    const int32_t *table;   /* [batch, table_ld], table_pages each     */
+    int64_t table_ld, table_pages, batch, new_tokens;
+} w4a8_kv_tokens;
+
+/* Quantizes the step's rows into the cache; rows i >= count[b] are not looked at.  No two positions of a step may share a place.
+ *   K, V   in   [batch, new_tokens, heads, head_dim] of dtype (F32, F16 or BF16), channels contiguous; k_ld, v_ld: distances
+ *               between sequences, tokens and heads, in elements
+ * and reads the same rows back as values, rounded once to dtype: K, V out, contiguous, 16-byte aligned, zeros where a sequence
+ * has no such token.  batch == 0 or new_tokens == 0 is a no-op for both. */
+int kv_cache_write_dint4(const void *K, const int64_t k_ld[3], const void *V, const int64_t v_ld[3], int dtype,
+                         const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens, void *stream);
+int kv_cache_read_dint4(const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens, void *K, void *V, int dtype, void *stream);
+
+/* Causal attention of the step's queries over the cache (the step's own tokens are in it already):
+ *     out[b,i,h] = sum_t p_t v_t,   p = softmax_t(scale * Q[b,i,h] . k_t),   t = 0 .. min(start[b] + i, max_len - 1),
+ * k, v: the rows of head h / (q_heads / heads).  Queries i >= count[b], and those that see no token, give zeros.
+ *   Q    in   [batch, new_tokens, q_heads, head_dim] of dtype, channels contiguous, q_ld as above; q_heads a multiple of heads
+ *   out       [batch, new_tokens, q_heads, head_dim] of dtype, contiguous, 16-byte aligned
+ *   max_len   what start[b] + count[b] is at most: work is divided by it, and tokens from there on are not seen
+ *   workspace of attention_kv_dint4_workspace_bytes(...) bytes, 256-byte aligned (NULL where that is 0): joined parts of
+ *             sequences that are cut; free for reuse once the call's work on `stream` has finished
+ * Scores and softmax are binary32; results do not depend on the order in which workgroups run. */
+size_t attention_kv_dint4_workspace_bytes(int dtype, int64_t q_heads, const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens,
+                                          int64_t max_len);
+int attention_kv_dint4(const void *Q, const int64_t q_ld[3], int dtype, int64_t q_heads, const w4a8_kv_cache *cache,
+                       const w4a8_kv_tokens *tokens, float scale, int64_t max_len, void *out, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
 /* Human-readable name of a status code (static storage, never NULL). */
 const char *w4a8_status_string(int status);
 

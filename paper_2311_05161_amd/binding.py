@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import importlib
 import os
+import typing
 import warnings
 
 import torch
@@ -40,6 +41,7 @@ EXPORTS = (
     "unpack_format",
     "dint_error_terms_workspace_bytes", "dint_error_terms",
     "expand_special_value", "w4a8_gemm_special_workspace_bytes", "w4a8_gemm_special",
+    "rms_norm_act_int8", "kv_cache_write_dint4", "kv_cache_read_dint4", "attention_kv_dint4", "attention_kv_dint4_workspace_bytes",
     "w4a8_measure_stream_read", "w4a8_measure_mfma_i8", "w4a8_measure_ktile_mix",
 )
 FMT_DINT4, FMT_INT4, FMT_DINT3, FMT_DINT4_C4, FMT_DINT4_C8 = 0, 1, 2, 3, 4
@@ -47,6 +49,16 @@ FMT_DINT4, FMT_INT4, FMT_DINT3, FMT_DINT4_C4, FMT_DINT4_C8 = 0, 1, 2, 3, 4
 _lib = None
 _native = None   # the native marshalling; False where it cannot be imported
 _addr = {}       # the addresses of the entry points that it calls (replaced as a whole, never filled in place)
+
+
+class _KVCacheArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_packed", "k_words", "v_packed", "v_words")] + \
+               [(n, ctypes.c_int64) for n in ("pages", "heads", "page_size", "head_dim")]
+
+
+class _KVTokensArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("start", "count", "table")] + \
+               [(n, ctypes.c_int64) for n in ("table_ld", "table_pages", "batch", "new_tokens")]
 
 
 class W4A8Error(RuntimeError):
@@ -147,6 +159,17 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     lib.dint_error_terms_workspace_bytes.restype = sz
     lib.dint_error_terms.argtypes = [vp, ci, i64, i64, i64, vp, ci, i64, i64, vp, i64, ci, vp, vp, sz, vp]
     lib.dint_error_terms.restype = ci
+    cache, tokens, ld = ctypes.POINTER(_KVCacheArgs), ctypes.POINTER(_KVTokensArgs), ctypes.POINTER(i64)
+    lib.rms_norm_act_int8.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, ci, ctypes.c_double, vp, vp, i64, vp, vp, vp]
+    lib.rms_norm_act_int8.restype = ci
+    lib.kv_cache_write_dint4.argtypes = [vp, ld, vp, ld, ci, cache, tokens, vp]
+    lib.kv_cache_write_dint4.restype = ci
+    lib.kv_cache_read_dint4.argtypes = [cache, tokens, vp, vp, ci, vp]
+    lib.kv_cache_read_dint4.restype = ci
+    lib.attention_kv_dint4_workspace_bytes.argtypes = [ci, i64, cache, tokens, i64]
+    lib.attention_kv_dint4_workspace_bytes.restype = sz
+    lib.attention_kv_dint4.argtypes = [vp, ld, ci, i64, cache, tokens, ctypes.c_float, i64, vp, vp, sz, vp]
+    lib.attention_kv_dint4.restype = ci
     lib.w4a8_status_string.argtypes = [ci]
     lib.w4a8_status_string.restype = ctypes.c_char_p
     global _native, _addr
@@ -155,7 +178,8 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     _addr = {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
              for name in ("quantize_act_int8", "quantize_act_int8_asym", "w4a8_gemm", "w4a8_gemm_asym", "w4a8_linear",
                           "w4a8_gemm_workspace_bytes", "w4a8_gemm_workspace_preferred_bytes", "w4a8_linear_workspace_bytes",
-                          "w4a8_linear_workspace_preferred_bytes")}
+                          "w4a8_linear_workspace_preferred_bytes", "rms_norm_act_int8", "kv_cache_write_dint4",
+                          "kv_cache_read_dint4", "attention_kv_dint4", "attention_kv_dint4_workspace_bytes")}
     _native = native
     _lib = lib
     return lib
@@ -640,3 +664,146 @@ def dint_error_terms(X: torch.Tensor, W: torch.Tensor, s=None, group_size: int =
                                            N, ldw, _ptr(s), int(group_size or 0), int(fmt), _ptr(terms),
                                            _ptr(ws), need, _stream()), "dint_error_terms")
     return terms
+
+
+# ---- around the layer in a decoder: the norm, the 4-bit cache of Keys and Values, attention over it ----
+def rms_norm_act_int8(x: torch.Tensor, w: torch.Tensor, eps: float = 1e-5, residual: torch.Tensor | None = None,
+                      s: torch.Tensor | None = None, h=None, Xq=None, sx=None):
+    """(Xq int8 [M,K], sx float32 [M]) = per-token absmax INT8 of the RMS norm of x (+ residual) diag(s)^-1; with a residual
+    also h = x + residual in x's type (``h`` may be given, also x or the residual itself)."""
+    if h is None and Xq is None and sx is None:
+        out = _native_call("rms_norm", "rms_norm_act_int8", _address("rms_norm_act_int8"), x, w, float(eps), residual, s)
+        if out is not NotImplemented:
+            return out
+    M, K, ldx = _rows(x, "x")
+    if w.shape != (K,) or not w.is_contiguous() or w.dtype not in (x.dtype, torch.float32) or w.device != x.device:
+        raise ValueError("w must be a contiguous vector of x's width and device, in x's type or float32")
+    if s is not None and (s.shape != (K,) or not s.is_contiguous() or s.dtype != torch.float32 or s.device != x.device):
+        raise ValueError("s must be a contiguous float32 vector of x's width, on x's device")
+    ldr = ldh = 0
+    if residual is not None:
+        _, _, ldr = _rows(residual, "residual")
+        if h is None:
+            h = torch.empty((M, K), dtype=x.dtype, device=x.device)
+        _, _, ldh = _rows(h, "h")
+        for t in (residual, h):
+            if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+                raise ValueError("residual and h must have x's shape, type and device")
+    elif h is not None:
+        raise ValueError("h is the sum with a residual: without one there is none")
+    if Xq is None:
+        Xq = torch.empty((M, K), dtype=torch.int8, device=x.device)
+    if sx is None:
+        sx = torch.empty((M,), dtype=torch.float32, device=x.device)
+    _check(load_library().rms_norm_act_int8(_ptr(x), _DTYPES[x.dtype], M, K, ldx, _ptr(residual), ldr, _ptr(w), _DTYPES[w.dtype],
+                                            float(eps), _ptr(s), _ptr(h), ldh, _ptr(Xq), _ptr(sx), _stream()), "rms_norm_act_int8")
+    return (Xq, sx, h) if residual is not None else (Xq, sx)
+
+
+class KVCacheDint4(typing.NamedTuple):
+    """The 4-bit cache of Keys and Values of a layer: packed uint8 [pages, heads, page_size, head_dim / 2], words int32
+    [pages, heads, page_size], both for Keys and for Values."""
+    k_packed: torch.Tensor
+    k_words: torch.Tensor
+    v_packed: torch.Tensor
+    v_words: torch.Tensor
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, device="cuda"):
+        """A cache with room for pages * page_size tokens; its contents are undefined until they are written."""
+        if head_dim % 8 != 0:
+            raise ValueError("head_dim must be a multiple of 8")
+        return cls(*(torch.empty((pages, heads, page_size, head_dim // 2), dtype=torch.uint8, device=device) if i % 2 == 0 else
+                     torch.empty((pages, heads, page_size), dtype=torch.int32, device=device) for i in range(4)))
+
+
+def _kv_args(cache, start, count, table):
+    """The two argument structs of the cache's entry points."""
+    kp = cache.k_packed
+    if kp.dim() != 4:
+        raise ValueError("packed rows must be [pages, heads, page_size, head_dim / 2]")
+    for t, want, dtype in ((cache.k_packed, kp.shape, torch.uint8), (cache.k_words, kp.shape[:3], torch.int32),
+                           (cache.v_packed, kp.shape, torch.uint8), (cache.v_words, kp.shape[:3], torch.int32)):
+        if t.shape != want or t.dtype != dtype or not t.is_contiguous() or t.device != kp.device:
+            raise ValueError("the cache's tensors must be contiguous, of one device and one set of pages: uint8 rows, int32 words")
+    if start.dim() != 1:
+        raise ValueError("start must be a vector, one number for each sequence")
+    B = start.shape[0]
+    for t in (start, count):
+        if t is not None and (t.shape != (B,) or t.dtype != torch.int32 or not t.is_contiguous() or t.device != kp.device):
+            raise ValueError("start and count must be contiguous int32 vectors of one length on the cache's device")
+    if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or table.device != kp.device or \
+            (table.stride(1) != 1 and table.shape[1] > 1):
+        raise ValueError("table must be int32 [sequences, pages] with contiguous rows, on the cache's device")
+    pages, heads, page_size, half = kp.shape
+    c = _KVCacheArgs(kp.data_ptr(), cache.k_words.data_ptr(), cache.v_packed.data_ptr(), cache.v_words.data_ptr(), pages, heads,
+                     page_size, 2 * half)
+    t = _KVTokensArgs(start.data_ptr(), None if count is None else count.data_ptr(), table.data_ptr(),
+                      table.stride(0) if B > 1 else max(table.stride(0), table.shape[1]), table.shape[1], B, 0)
+    return c, t
+
+
+def _kv_rows(x, what, c, t, device):
+    if x.dim() != 4 or x.shape[0] != t.batch or x.shape[3] != c.head_dim or x.stride(3) != 1 or x.device != device:
+        raise ValueError(f"{what} must be [sequences, tokens, heads, head_dim] with contiguous channels, on the cache's device")
+    return (ctypes.c_int64 * 3)(*(x.stride(i) if x.shape[i] > 1 else 0 for i in range(3)))
+
+
+def kv_cache_write_dint4(k: torch.Tensor, v: torch.Tensor, cache: KVCacheDint4, start: torch.Tensor,
+                         count: torch.Tensor | None, table: torch.Tensor) -> None:
+    """Quantizes Keys and Values k, v [B, S, heads, D] into the cache, token i of sequence b at position start[b] + i for
+    i < count[b] (None: all S); position p lies in page table[b, p // page_size]."""
+    out = _native_call("kv_write", "kv_cache_write_dint4", _address("kv_cache_write_dint4"), k, v, *cache, start, count, table)
+    if out is not NotImplemented:
+        return
+    c, t = _kv_args(cache, start, count, table)
+    k_ld, v_ld = (_kv_rows(x, n, c, t, cache.k_packed.device) for x, n in ((k, "k"), (v, "v")))
+    if k.shape != v.shape or k.dtype != v.dtype or k.shape[2] != c.heads:
+        raise ValueError("k and v must have one type and shape, with the cache's heads")
+    t.new_tokens = k.shape[1]
+    _check(load_library().kv_cache_write_dint4(_ptr(k), k_ld, _ptr(v), v_ld, _DTYPES[k.dtype], c, t, _stream()),
+           "kv_cache_write_dint4")
+
+
+def kv_cache_read_dint4(cache: KVCacheDint4, start: torch.Tensor, new_tokens: int, count: torch.Tensor | None, table: torch.Tensor,
+                        dtype=torch.float16):
+    """(k, v) [B, new_tokens, heads, D]: the values that the cache holds at positions start[b] .. start[b] + count[b] - 1, zeros
+    behind them."""
+    out = _native_call("kv_read", "kv_cache_read_dint4", _address("kv_cache_read_dint4"), *cache, start, count, table, new_tokens,
+                       _DTYPES[dtype])
+    if out is not NotImplemented:
+        return out
+    c, t = _kv_args(cache, start, count, table)
+    if new_tokens < 0:
+        raise ValueError("new_tokens must not be negative")
+    t.new_tokens = new_tokens
+    k, v = (torch.empty((t.batch, new_tokens, c.heads, c.head_dim), dtype=dtype, device=cache.k_packed.device) for _ in range(2))
+    _check(load_library().kv_cache_read_dint4(c, t, _ptr(k), _ptr(v), _DTYPES[dtype], _stream()), "kv_cache_read_dint4")
+    return k, v
+
+
+def attention_kv_dint4(q: torch.Tensor, cache: KVCacheDint4, start: torch.Tensor, count: torch.Tensor | None, table: torch.Tensor,
+                       scale: float | None = None, max_len: int | None = None) -> torch.Tensor:
+    """Causal attention of q [B, S, q_heads, D], the newest tokens (already in the cache), over the cache: [B, S, q_heads, D].
+
+    Query i of sequence b sees positions 0 .. start[b] + i; queries i >= count[b] give zeros.  ``scale``: 1 / sqrt(D) if not
+    given.  ``max_len``: what start[b] + count[b] is at most, by which the work is divided (tokens from there on are not
+    seen); if not given, what the table has room for."""
+    if scale is None:
+        scale = q.shape[-1] ** -0.5
+    if max_len is None:
+        max_len = table.shape[-1] * cache.k_packed.shape[2]
+    out = _native_call("kv_attention", "attention_kv_dint4", _address("attention_kv_dint4"),
+                       _address("attention_kv_dint4_workspace_bytes"), q, *cache, start, count, table, float(scale), max_len)
+    if out is not NotImplemented:
+        return out
+    c, t = _kv_args(cache, start, count, table)
+    q_ld = _kv_rows(q, "q", c, t, cache.k_packed.device)
+    t.new_tokens = q.shape[1]
+    lib, dtype = load_library(), _DTYPES[q.dtype]
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    need = int(lib.attention_kv_dint4_workspace_bytes(dtype, q.shape[2], c, t, int(max_len)))
+    ws = torch.empty((need,), dtype=torch.uint8, device=q.device) if need > 0 else None
+    _check(lib.attention_kv_dint4(_ptr(q), q_ld, dtype, q.shape[2], c, t, float(scale), int(max_len), _ptr(out), _ptr(ws), need,
+                                  _stream()), "attention_kv_dint4")
+    return out

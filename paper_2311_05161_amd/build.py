@@ -21,6 +21,9 @@ NATIVE_PATH = os.path.join(HERE, "_native.so")
 SOURCES = {
     "api.hip": [],
     "act_quant.hip": ["-ffp-contract=off"],
+    "norm_quant.hip": ["-ffp-contract=off"],
+    "kv_cache.hip": ["-ffp-contract=off"],
+    "attention_kv.hip": [],
     "weight_quant.hip": ["-ffp-contract=off"],
     "pack.hip": [],
     "gemm_decode.hip": [],

@@ -2,7 +2,7 @@
 // no synchronization; every error is reported before anything is launched.
 #include <algorithm>
 
-#include "w4a8_common.hpp"
+#include "kv_dint4.hpp"
 
 using namespace w4a8;
 
@@ -193,6 +193,100 @@ int quantize_act_int8_asym(const void *X, int x_dtype, int64_t M, int64_t K, int
     if (M == 0) return W4A8_OK;
     if (!X || !Xq || !sx || !zx) return W4A8_ERR_NULL;
     return launch_act_quant(X, x_dtype, M, K, ldx, s, Xq, sx, zx, (hipStream_t)stream);
+}
+
+int rms_norm_act_int8(const void *X, int x_dtype, int64_t M, int64_t K, int64_t ldx, const void *R, int64_t ldr, const void *w,
+                      int w_dtype, double eps, const float *s, void *H, int64_t ldh, int8_t *Xq, float *sx, void *stream)
+{
+    if (!valid_dtype(x_dtype) || (w_dtype != x_dtype && w_dtype != W4A8_F32)) return W4A8_ERR_DTYPE;
+    if (M < 0 || K < 1 || ldx < K || M > 0x7fffffffLL || K > 0x7fffffLL || !(eps >= 0.0)) return W4A8_ERR_SHAPE;
+    if (R && (ldr < K || ldh < K)) return W4A8_ERR_SHAPE;
+    if (M == 0) return W4A8_OK;
+    if (!X || !w || !Xq || !sx || (R && !H)) return W4A8_ERR_NULL;
+    return launch_norm_quant(X, x_dtype, M, K, ldx, R, ldr, w, w_dtype, s, eps, R ? H : nullptr, ldh, Xq, sx, (hipStream_t)stream);
+}
+
+// What the entry points of the 4-bit cache have in common: the shapes, before any pointer is looked at.
+static int kv_shape(const w4a8_kv_cache *c, const w4a8_kv_tokens *t)
+{
+    if (!c || !t) return W4A8_ERR_NULL;
+    if (c->pages < 0 || c->heads < 1 || c->heads > 65535 || c->page_size < 1 || c->page_size > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+    if (c->head_dim < 8 || c->head_dim > 512 || c->head_dim % 8 != 0 || c->pages > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+    if (t->batch < 0 || t->batch > 0x7fffffffLL || t->new_tokens < 0 || t->table_pages < 0 || t->table_ld < t->table_pages) return W4A8_ERR_SHAPE;
+    // (positions are numbered in 32 bits, and the step's tokens are part of them)
+    if (t->table_pages > 0x7fffffffLL / c->page_size || t->new_tokens > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+    return W4A8_OK;
+}
+static bool kv_empty(const w4a8_kv_tokens *t) { return t->batch == 0 || t->new_tokens == 0; }
+// (a table of no pages is never looked at, nor are the rows of a cache of no pages)
+static int kv_pointers(const w4a8_kv_cache *c, const w4a8_kv_tokens *t)
+{
+    if (!t->start || (t->table_pages > 0 && !t->table)) return W4A8_ERR_NULL;
+    if (c->pages > 0 && (!c->k_packed || !c->k_words || !c->v_packed || !c->v_words)) return W4A8_ERR_NULL;
+    if (((uintptr_t)c->k_packed | (uintptr_t)c->v_packed) % 16 != 0 || ((uintptr_t)c->k_words | (uintptr_t)c->v_words) % 16 != 0) return W4A8_ERR_SHAPE;
+    return W4A8_OK;
+}
+static KvView kv_view(const w4a8_kv_cache *c)
+{
+    return {{c->k_packed, c->v_packed}, {c->k_words, c->v_words}, c->pages, (int)c->heads, (int)c->page_size, (int)c->head_dim};
+}
+static KvTokens kv_tokens(const w4a8_kv_tokens *t)
+{
+    return {t->start, t->count, t->table, t->table_ld, (int)t->batch, (int)t->new_tokens, (int)t->table_pages};
+}
+
+int kv_cache_write_dint4(const void *K, const int64_t k_ld[3], const void *V, const int64_t v_ld[3], int dtype,
+                         const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens, void *stream)
+{
+    if (!valid_dtype(dtype)) return W4A8_ERR_DTYPE;
+    int rc = kv_shape(cache, tokens);
+    if (rc != W4A8_OK || kv_empty(tokens)) return rc;
+    if (!K || !V || !k_ld || !v_ld) return W4A8_ERR_NULL;
+    if ((rc = kv_pointers(cache, tokens)) != W4A8_OK) return rc;
+    return launch_kv_cache(true, K, k_ld, V, v_ld, dtype, kv_view(cache), kv_tokens(tokens), (hipStream_t)stream);
+}
+
+int kv_cache_read_dint4(const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens, void *K, void *V, int dtype, void *stream)
+{
+    if (!valid_dtype(dtype)) return W4A8_ERR_DTYPE;
+    int rc = kv_shape(cache, tokens);
+    if (rc != W4A8_OK || kv_empty(tokens)) return rc;
+    if (!K || !V) return W4A8_ERR_NULL;
+    if ((rc = kv_pointers(cache, tokens)) != W4A8_OK) return rc;
+    if (((uintptr_t)K | (uintptr_t)V) % 16 != 0) return W4A8_ERR_SHAPE;
+    const int64_t ld[3] = {tokens->new_tokens * cache->heads * cache->head_dim, cache->heads * cache->head_dim, cache->head_dim};
+    return launch_kv_cache(false, K, ld, V, ld, dtype, kv_view(cache), kv_tokens(tokens), (hipStream_t)stream);
+}
+
+static int attention_shape(int64_t q_heads, int dtype, const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens, int64_t max_len)
+{
+    if (!valid_dtype(dtype)) return W4A8_ERR_DTYPE;
+    const int rc = kv_shape(cache, tokens);
+    if (rc != W4A8_OK) return rc;
+    if (q_heads < 1 || q_heads > 0x7fffffLL || q_heads % cache->heads != 0 || max_len < 0) return W4A8_ERR_SHAPE;
+    return W4A8_OK;
+}
+
+size_t attention_kv_dint4_workspace_bytes(int dtype, int64_t q_heads, const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens,
+                                          int64_t max_len)
+{
+    if (attention_shape(q_heads, dtype, cache, tokens, max_len) != W4A8_OK || kv_empty(tokens)) return 0;
+    return attention_kv_workspace(dtype, kv_view(cache), kv_tokens(tokens), (int)q_heads, max_len);
+}
+
+int attention_kv_dint4(const void *Q, const int64_t q_ld[3], int dtype, int64_t q_heads, const w4a8_kv_cache *cache,
+                       const w4a8_kv_tokens *tokens, float scale, int64_t max_len, void *out, void *workspace,
+                       size_t workspace_bytes, void *stream)
+{
+    int rc = attention_shape(q_heads, dtype, cache, tokens, max_len);
+    if (rc != W4A8_OK || kv_empty(tokens)) return rc;
+    if (!Q || !q_ld || !out) return W4A8_ERR_NULL;
+    if ((rc = kv_pointers(cache, tokens)) != W4A8_OK) return rc;
+    if ((uintptr_t)out % 16 != 0) return W4A8_ERR_SHAPE;
+    const size_t need = attention_kv_workspace(dtype, kv_view(cache), kv_tokens(tokens), (int)q_heads, max_len);
+    if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % WS_ALIGN != 0)) return W4A8_ERR_WORKSPACE;
+    return launch_attention_kv(Q, q_ld, dtype, (int)q_heads, kv_view(cache), kv_tokens(tokens), scale, max_len, out, workspace,
+                               (hipStream_t)stream);
 }
 
 int dint4_weight_sums(const uint8_t *codes, const uint8_t *zero, int64_t N, int64_t K,

@@ -278,7 +278,191 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
+// rms_norm(entry, X, w, eps, residual, s, stream) -> (Xq, sx) or (Xq, sx, h)
+PyObject *rms_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 7 || !plain(a[1]) || !plain(a[2]) || !PyFloat_Check(a[3]) || !plain_or_none(a[4]) || !plain_or_none(a[5])) return not_implemented();
+    decltype(&rms_norm_act_int8) entry;
+    int64_t stream;
+    if (!to_fn(a[0], entry)) return nullptr;
+    if (!to_i64(a[6], stream)) return not_implemented();
+    const at::Tensor &X = THPVariable_Unpack(a[1]), &w = THPVariable_Unpack(a[2]);
+    const Rows r = rows_of(X);
+    const int wd = dtype_id(w.scalar_type());
+    if (!r.ok || wd < 0 || w.dim() != 1 || w.size(0) != r.K || !w.is_contiguous() || w.device() != X.device()) return not_implemented();
+    const float *s = nullptr;
+    if (a[5] != Py_None) {
+        const at::Tensor &st = THPVariable_Unpack(a[5]);
+        if (st.scalar_type() != at::kFloat || st.dim() != 1 || st.size(0) != r.K || !st.is_contiguous() || st.device() != X.device()) return not_implemented();
+        s = (const float *)st.data_ptr();
+    }
+    at::Tensor h;
+    Rows rr{0, 0, 0, -1, false};
+    const void *res = nullptr;
+    if (a[4] != Py_None) {
+        const at::Tensor &R = THPVariable_Unpack(a[4]);
+        rr = rows_of(R);
+        if (!rr.ok || rr.M != r.M || rr.K != r.K || rr.dtype != r.dtype || R.device() != X.device()) return not_implemented();
+        res = R.data_ptr();
+        h = make(X, {r.M, r.K}, X.scalar_type());
+    }
+    at::Tensor Xq = make(X, {r.M, r.K}, at::kChar), sx = make(X, {r.M}, at::kFloat);
+    const void *x = X.data_ptr(), *wp = w.data_ptr();
+    void *hp = data(h);
+    int8_t *q = (int8_t *)Xq.data_ptr();
+    float *sxp = (float *)sx.data_ptr();
+    const double eps = PyFloat_AS_DOUBLE(a[3]);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = entry(x, r.dtype, r.M, r.K, r.ld, res, rr.ld, wp, wd, eps, s, hp, r.K, q, sxp, (void *)stream);
+    Py_END_ALLOW_THREADS
+    if (rc != W4A8_OK) return status(rc);
+    py::object o0 = py::reinterpret_steal<py::object>(THPVariable_Wrap(Xq)), o1 = py::reinterpret_steal<py::object>(THPVariable_Wrap(sx));
+    if (!h.defined()) return PyTuple_Pack(2, o0.ptr(), o1.ptr());
+    py::object o2 = py::reinterpret_steal<py::object>(THPVariable_Wrap(h));
+    return PyTuple_Pack(3, o0.ptr(), o1.ptr(), o2.ptr());
+    END_HANDLE_TH_ERRORS
+}
+
+// The cache (four tensors) and the step's start, count, table: false where they are not what the entry points take.
+bool kv_operands(PyObject *const *c, PyObject *const *t, w4a8_kv_cache &cache, w4a8_kv_tokens &tok, c10::Device &device)
+{
+    for (int i = 0; i < 4; ++i)
+        if (!plain(c[i])) return false;
+    if (!plain(t[0]) || !plain_or_none(t[1]) || !plain(t[2])) return false;
+    const at::Tensor &kp = THPVariable_Unpack(c[0]);
+    if (kp.dim() != 4) return false;
+    device = kp.device();
+    cache.pages = kp.size(0);
+    cache.heads = kp.size(1);
+    cache.page_size = kp.size(2);
+    cache.head_dim = 2 * kp.size(3);
+    for (int i = 0; i < 4; ++i) {
+        const at::Tensor &x = THPVariable_Unpack(c[i]);
+        const bool words = i & 1;
+        if (x.dim() != (words ? 3 : 4) || !x.is_contiguous() || x.scalar_type() != (words ? at::kInt : at::kByte) || x.device() != device) return false;
+        for (int d = 0; d < x.dim(); ++d)
+            if (x.size(d) != kp.size(d)) return false;
+    }
+    cache.k_packed = (uint8_t *)kp.data_ptr();
+    cache.k_words = (int32_t *)ptr(c[1]);
+    cache.v_packed = (uint8_t *)ptr(c[2]);
+    cache.v_words = (int32_t *)ptr(c[3]);
+    const at::Tensor &start = THPVariable_Unpack(t[0]), &table = THPVariable_Unpack(t[2]);
+    tok.batch = start.dim() == 1 ? start.size(0) : -1;
+    const auto vec = [&](const at::Tensor &x) { return x.dim() == 1 && x.size(0) == tok.batch && x.scalar_type() == at::kInt && x.is_contiguous() && x.device() == device; };
+    if (!vec(start) || (t[1] != Py_None && !vec(THPVariable_Unpack(t[1])))) return false;
+    if (table.dim() != 2 || table.size(0) != tok.batch || table.scalar_type() != at::kInt || table.device() != device) return false;
+    if (table.stride(1) != 1 && table.size(1) > 1) return false;
+    tok.start = (const int32_t *)start.data_ptr();
+    tok.count = (const int32_t *)ptr(t[1]);
+    tok.table = (const int32_t *)table.data_ptr();
+    tok.table_pages = table.size(1);
+    tok.table_ld = tok.batch > 1 ? table.stride(0) : std::max(table.stride(0), table.size(1));
+    return true;
+}
+
+// [batch, tokens, heads, channels] with the channels contiguous
+bool kv_rows(const at::Tensor &x, const w4a8_kv_cache &cache, const w4a8_kv_tokens &tok, const c10::Device &device, int64_t (&ld)[3])
+{
+    if (x.dim() != 4 || x.size(0) != tok.batch || x.size(3) != cache.head_dim || x.stride(3) != 1 || x.device() != device) return false;
+    for (int i = 0; i < 3; ++i) ld[i] = x.size(i) > 1 ? x.stride(i) : 0;
+    return dtype_id(x.scalar_type()) >= 0;
+}
+
+// kv_write(entry, K, V, k_packed, k_words, v_packed, v_words, start, count, table, stream) -> None
+PyObject *kv_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    decltype(&kv_cache_write_dint4) entry;
+    int64_t stream, k_ld[3], v_ld[3];
+    w4a8_kv_cache cache;
+    w4a8_kv_tokens tok;
+    c10::Device device(c10::kCPU);
+    if (n != 11 || !plain(a[1]) || !plain(a[2]) || !kv_operands(a + 3, a + 7, cache, tok, device)) return not_implemented();
+    if (!to_fn(a[0], entry)) return nullptr;
+    if (!to_i64(a[10], stream)) return not_implemented();
+    const at::Tensor &K = THPVariable_Unpack(a[1]), &V = THPVariable_Unpack(a[2]);
+    if (!kv_rows(K, cache, tok, device, k_ld) || !kv_rows(V, cache, tok, device, v_ld) || K.sizes() != V.sizes() ||
+        K.size(2) != cache.heads || K.scalar_type() != V.scalar_type())
+        return not_implemented();
+    tok.new_tokens = K.size(1);
+    const void *k = K.data_ptr(), *v = V.data_ptr();
+    const int dtype = dtype_id(K.scalar_type());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = entry(k, k_ld, v, v_ld, dtype, &cache, &tok, (void *)stream);
+    Py_END_ALLOW_THREADS
+    if (rc != W4A8_OK) return status(rc);
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_read(entry, k_packed, k_words, v_packed, v_words, start, count, table, new_tokens, dtype, stream) -> (K, V)
+PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    decltype(&kv_cache_read_dint4) entry;
+    int64_t S, dtype, stream;
+    w4a8_kv_cache cache;
+    w4a8_kv_tokens tok;
+    c10::Device device(c10::kCPU);
+    if (n != 11 || !kv_operands(a + 1, a + 5, cache, tok, device)) return not_implemented();
+    if (!to_fn(a[0], entry)) return nullptr;
+    if (!to_i64(a[8], S) || !to_i64(a[9], dtype) || !to_i64(a[10], stream) || S < 0) return not_implemented();
+    tok.new_tokens = S;
+    const at::Tensor &like = THPVariable_Unpack(a[1]);
+    const int64_t size[4] = {tok.batch, S, cache.heads, cache.head_dim};
+    at::Tensor K = make(like, size, y_type(dtype)), V = make(like, size, y_type(dtype));
+    void *k = K.data_ptr(), *v = V.data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = entry(&cache, &tok, k, v, (int)dtype, (void *)stream);
+    Py_END_ALLOW_THREADS
+    if (rc != W4A8_OK) return status(rc);
+    return PyTuple_Pack(2, py::reinterpret_steal<py::object>(THPVariable_Wrap(K)).ptr(),
+                        py::reinterpret_steal<py::object>(THPVariable_Wrap(V)).ptr());
+    END_HANDLE_TH_ERRORS
+}
+
+// kv_attention(entry, workspace_entry, Q, k_packed, k_words, v_packed, v_words, start, count, table, scale, max_len, stream) -> out
+PyObject *kv_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    decltype(&attention_kv_dint4) entry;
+    decltype(&attention_kv_dint4_workspace_bytes) need;
+    int64_t max_len, stream, q_ld[3];
+    w4a8_kv_cache cache;
+    w4a8_kv_tokens tok;
+    c10::Device device(c10::kCPU);
+    if (n != 13 || !plain(a[2]) || !kv_operands(a + 3, a + 7, cache, tok, device) || !PyFloat_Check(a[10])) return not_implemented();
+    if (!to_fn(a[0], entry) || !to_fn(a[1], need)) return nullptr;
+    if (!to_i64(a[11], max_len) || !to_i64(a[12], stream)) return not_implemented();
+    const at::Tensor &Q = THPVariable_Unpack(a[2]);
+    if (!kv_rows(Q, cache, tok, device, q_ld)) return not_implemented();
+    tok.new_tokens = Q.size(1);
+    const int64_t heads = Q.size(2);
+    const int dtype = dtype_id(Q.scalar_type());
+    at::Tensor out = make(Q, Q.sizes(), Q.scalar_type()), ws;
+    const size_t bytes = need(dtype, heads, &cache, &tok, max_len);
+    if (bytes > 0) ws = make(Q, {(int64_t)bytes}, at::kByte);
+    const void *q = Q.data_ptr();
+    void *o = out.data_ptr(), *w = data(ws);
+    const float scale = (float)PyFloat_AS_DOUBLE(a[10]);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = entry(q, q_ld, dtype, heads, &cache, &tok, scale, max_len, o, w, bytes, (void *)stream);
+    Py_END_ALLOW_THREADS
+    return rc != W4A8_OK ? status(rc) : THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
+    {"rms_norm", (PyCFunction)(void (*)(void))rms_norm, METH_FASTCALL, nullptr},
+    {"kv_write", (PyCFunction)(void (*)(void))kv_write, METH_FASTCALL, nullptr},
+    {"kv_read", (PyCFunction)(void (*)(void))kv_read, METH_FASTCALL, nullptr},
+    {"kv_attention", (PyCFunction)(void (*)(void))kv_attention, METH_FASTCALL, nullptr},
     {"act_quant", (PyCFunction)(void (*)(void))act_quant, METH_FASTCALL, nullptr},
     {"act_quant_asym", (PyCFunction)(void (*)(void))act_quant_asym, METH_FASTCALL, nullptr},
     {"gemm", (PyCFunction)(void (*)(void))gemm, METH_FASTCALL, nullptr},

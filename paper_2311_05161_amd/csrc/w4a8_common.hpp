@@ -220,6 +220,9 @@ __device__ __forceinline__ void decode_word_signed(uint32_t p, const SignedLut &
 int launch_act_quant(const void *X, int x_dtype, int64_t M, int64_t K, int64_t ldx, const float *s,
                      int8_t *Xq, float *sx, int32_t *zx, hipStream_t st, int32_t *rs = nullptr);
 bool act_quant_sums_rows(const void *X, int x_dtype, int64_t K, int64_t ldx, const float *s, const int8_t *Xq);
+// root-mean-square norm with the residual's addition, straight to int8 (norm_quant.hip); R, H, s may be null
+int launch_norm_quant(const void *X, int x_dtype, int64_t M, int64_t K, int64_t ldx, const void *R, int64_t ldr, const void *w,
+                      int w_dtype, const float *s, double eps, void *H, int64_t ldh, int8_t *Xq, float *sx, hipStream_t st);
 // sums of the weights in half steps: wsum [N, K/G] per group, tsum [N, K/128] per 128 columns (or null)
 int launch_weight_sums(const uint8_t *codes, const uint8_t *zero, int64_t N, int64_t K, int64_t G,
                        int32_t *wsum, int32_t *tsum, hipStream_t st);

@@ -1,0 +1,127 @@
+"""The norm, the 4-bit cache and attention over it from their definitions, in float64 on the CPU (torch only)."""
+import math
+
+import torch
+
+TORCH_DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF_STEP = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}   # of a rounding, relative
+
+
+def channel_bytes(D):
+    """Byte and shift of every channel's nibble in a packed row."""
+    c = torch.arange(D)
+    return c // 8 * 4 + c % 4, (c % 8) // 4 * 4
+
+
+def values64(packed, words):
+    """float64 values [..., D] of packed rows [..., D/2] under their words [...]."""
+    byte, shift = channel_bytes(2 * packed.shape[-1])
+    e = (packed.to(torch.int64)[..., byte] >> shift) & 15
+    step = (words & -16).view(torch.float32).double()
+    z = (words & 15).to(torch.int64)
+    low, high = e & 7, e >> 3
+    half_steps = torch.where(low == 7, 2 * high - 1, 2 * (2 * low + high) - 2 * z[..., None])
+    return half_steps.double() * (step / 2)[..., None]
+
+
+def round_step(x):
+    """float64 -> 20 significant bits, half up; 0 below the smallest normal binary32 number."""
+    m, e = torch.frexp(x)
+    s = torch.floor(m * 2.0 ** 20 + 0.5) * torch.exp2((e - 20).double())
+    return torch.where(s >= 2.0 ** -126, s, torch.zeros_like(s))
+
+
+def quantize64(x):
+    """Packed rows and words of x [..., D]: the rule in exact arithmetic (for 16-bit x)."""
+    x = x.double()
+    D = x.shape[-1]
+    lo, hi = x.amin(-1).clamp(max=0), x.amax(-1).clamp(min=0)
+    step = round_step((hi - lo) / 13)
+    safe = torch.where(step > 0, step, torch.ones_like(step))
+    z = torch.where(step > 0, torch.round(-lo / safe).clamp(0, 13), torch.zeros_like(step))
+    u = torch.where((step > 0)[..., None], x / safe[..., None], torch.zeros_like(x))
+    code = (torch.round(u) + z[..., None]).clamp(0, 13).to(torch.int64)
+    e = (code >> 1) | (code & 1) << 3
+    e = torch.where((u > 0.25) & (u <= 0.75), 15, e)
+    e = torch.where((u < -0.25) & (u >= -0.75), 7, e)
+    byte, shift = channel_bytes(D)
+    packed = torch.zeros((*x.shape[:-1], D // 2), dtype=torch.int64)
+    packed.index_add_(-1, byte, e << shift)
+    return packed.to(torch.uint8), step.float().view(torch.int32) | z.to(torch.int32)
+
+
+def lengths(start, count, S, room):
+    start = [min(max(int(v), 0), room) for v in start]
+    count = [S if count is None else min(max(int(c), 0), S, room - s) for s, c in zip(start, count if count is not None else start)]
+    return start, [min(c, room - s) for s, c in zip(start, count)]
+
+
+def gather(cache, table_row, n):
+    """The rows of positions 0 .. n - 1 of a sequence: K, V float64 [heads, n, D], and which of them are in the cache."""
+    kp, kw, vp, vw = cache
+    P = kp.shape[2]
+    pos = torch.arange(n)
+    page = table_row[pos // P].to(torch.int64)
+    good = (page >= 0) & (page < kp.shape[0])
+    page = torch.where(good, page, 0)
+    K = values64(kp[page, :, pos % P], kw[page, :, pos % P])
+    V = values64(vp[page, :, pos % P], vw[page, :, pos % P])
+    K, V = torch.where(good[:, None, None], K, 0.0), torch.where(good[:, None, None], V, 0.0)
+    return K.transpose(0, 1), V.transpose(0, 1), good
+
+
+def attention64(q, cache, start, count, table, scale, max_len=None):
+    """out [B, S, Hq, D] float64 and the bound of its error (see attention_bound)."""
+    B, S, Hq, D = q.shape
+    H, P = cache[0].shape[1], cache[0].shape[2]
+    room = table.shape[1] * P
+    start, count = lengths(start, count, S, room)
+    out, slack = torch.zeros((B, S, Hq, D), dtype=torch.float64), torch.zeros((B, S, Hq, D), dtype=torch.float64)
+    for b in range(B):
+        n = start[b] + count[b]
+        if n == 0:
+            continue
+        K, V, good = gather(cache, table[b], n)
+        K, V = K.repeat_interleave(Hq // H, 0), V.repeat_interleave(Hq // H, 0)
+        pos = torch.arange(n)
+        if max_len is not None:
+            good = good & (pos < max_len)
+        Q = q[b, : count[b]].double().transpose(0, 1)                       # [Hq, c, D]
+        score = torch.matmul(Q, K.transpose(1, 2)) * scale
+        seen = good[None] & (pos[None] <= start[b] + torch.arange(count[b])[:, None])
+        score = score.masked_fill(~seen[None], -math.inf)
+        p = torch.softmax(score, -1)
+        p = torch.where(seen.any(-1)[None, :, None], p, 0.0)
+        out[b, : count[b]] = torch.matmul(p, V).transpose(0, 1)
+        # binary32 scores: at most D additions of terms that are at most |q| times 28 half steps, each rounded relative to the
+        # sum so far; in products of 16 to 64 terms at a time, so 16 roundings of the largest sum bound them
+        top = 14.0 * Q.abs().sum(-1) * abs(scale) * (K.abs().amax(-1).amax(-1) / 1.0)[:, None]
+        err = 2.0 ** -20 * top
+        slack[b, : count[b]] = (torch.matmul(p, V.abs()) * (2.0 ** -11 + 2 * err[..., None] + 2.0 ** -19)).transpose(0, 1)
+    return out, slack
+
+
+def assert_attention(got, ref, slack, where=""):
+    """|got - ref| <= half a step of the output's type + what the weights' rounding to 11 bits, the binary32 scores and
+    exponentials (2^-20 each) leave of sum p |v|, + half the smallest step of fp16."""
+    bound = HALF_STEP[got.dtype] * (ref.abs() + slack) + slack + 2.0 ** -25
+    err = (got.double().cpu() - ref).abs()
+    bad = ~(err <= bound)
+    assert not bad.any(), f"{where}: {int(bad.sum())} of {bad.numel()} off; worst {float((err / bound).nan_to_num(1e9).max()):.3g} x the bound at " \
+                          f"{(err / bound).nan_to_num(1e9).argmax()}"
+
+
+def random_cache(g, pages, H, P, D, spread=1.0):
+    """A cache of random rows: every code, zero-points 0 .. 13, unequal steps."""
+    out = []
+    for gain in (0.2, 0.1):
+        packed = torch.randint(0, 256, (pages, H, P, D // 2), generator=g, dtype=torch.uint8)
+        step = round_step((torch.exp2(spread * torch.randn((pages, H, P), generator=g).double()) * gain)).float()
+        z = torch.randint(0, 14, (pages, H, P), generator=g, dtype=torch.int32)
+        out += [packed, step.view(torch.int32) | z]
+    return out
+
+
+def random_tables(g, B, each, pages):
+    """Distinct pages for every sequence, in no order."""
+    return torch.randperm(pages, generator=g)[: B * each].reshape(B, each).to(torch.int32)

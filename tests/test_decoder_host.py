@@ -1,0 +1,129 @@
+"""Host-side checks, without a GPU, of the norm, the 4-bit cache and its attention: what they refuse, and that the float64
+definitions the GPU tests compare with agree with the weights' own oracle."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import decoder_util as du
+import paper_2311_05161_amd as w
+from paper_2311_05161_amd import binding as b
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return w.load_library()
+
+
+P16 = ctypes.c_void_p(0x1000)    # never touched
+Z = ctypes.c_void_p(0)
+
+
+def cache_args(**kw):
+    d = dict(k_packed=0x1000, k_words=0x2000, v_packed=0x3000, v_words=0x4000, pages=8, heads=4, page_size=16, head_dim=128)
+    return b._KVCacheArgs(**{**d, **kw})
+
+
+def token_args(**kw):
+    d = dict(start=0x1000, count=0x2000, table=0x3000, table_ld=4, table_pages=4, batch=2, new_tokens=3)
+    return b._KVTokensArgs(**{**d, **kw})
+
+
+LD = (ctypes.c_int64 * 3)(3 * 512, 512, 128)
+
+
+def test_norm_refusals(lib):
+    f = lib.rms_norm_act_int8
+    ok = dict(X=P16, xd=b.F16, M=2, K=64, ldx=64, R=P16, ldr=64, w=P16, wd=b.F16, eps=1e-5, s=Z, H=P16, ldh=64, Xq=P16, sx=P16)
+
+    def call(**kw):
+        return f(*{**ok, **kw}.values(), Z)
+
+    assert call(xd=7) == call(xd=-1) == call(wd=b.BF16) == b.ERR_DTYPE
+    assert call(K=0) == call(M=-1) == call(ldx=63) == call(ldr=63) == call(ldh=63) == b.ERR_SHAPE
+    assert call(eps=-1.0) == call(eps=float("nan")) == b.ERR_SHAPE
+    assert call(X=Z) == call(w=Z) == call(H=Z) == call(Xq=Z) == call(sx=Z) == b.ERR_NULL
+    assert call(M=0, X=Z) == b.OK
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(heads=0), b.ERR_SHAPE), (dict(page_size=0), b.ERR_SHAPE), (dict(head_dim=0), b.ERR_SHAPE), (dict(head_dim=60), b.ERR_SHAPE),
+    (dict(head_dim=520), b.ERR_SHAPE), (dict(pages=-1), b.ERR_SHAPE), (dict(page_size=1 << 30), b.ERR_SHAPE),
+    (dict(k_packed=0), b.ERR_NULL), (dict(v_words=0), b.ERR_NULL), (dict(k_packed=0x1008), b.ERR_SHAPE), (dict(v_words=0x4004), b.ERR_SHAPE)])
+def test_cache_refusals(lib, bad, status):
+    c, t = cache_args(**bad), token_args()
+    assert lib.kv_cache_write_dint4(P16, LD, P16, LD, b.F16, c, t, Z) == status
+    assert lib.kv_cache_read_dint4(c, t, P16, P16, b.F16, Z) == status
+    assert lib.attention_kv_dint4(P16, LD, b.F16, c.heads * 2, c, t, 1.0, 64, P16, Z, 0, Z) == status
+    if status == b.ERR_SHAPE and "k_packed" not in bad and "v_words" not in bad:
+        assert lib.attention_kv_dint4_workspace_bytes(b.F16, c.heads * 2, c, t, 64) == 0
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(batch=-1), b.ERR_SHAPE), (dict(new_tokens=-1), b.ERR_SHAPE), (dict(table_ld=3), b.ERR_SHAPE), (dict(table_pages=-1), b.ERR_SHAPE),
+    (dict(table_ld=1 << 40, table_pages=1 << 40), b.ERR_SHAPE), (dict(start=0), b.ERR_NULL), (dict(table=0), b.ERR_NULL)])
+def test_token_refusals(lib, bad, status):
+    c, t = cache_args(), token_args(**bad)
+    assert lib.kv_cache_write_dint4(P16, LD, P16, LD, b.F16, c, t, Z) == status
+    assert lib.kv_cache_read_dint4(c, t, P16, P16, b.F16, Z) == status
+    assert lib.attention_kv_dint4(P16, LD, b.F16, 8, c, t, 1.0, 64, P16, Z, 0, Z) == status
+
+
+def test_other_refusals_and_empty_calls(lib):
+    c, t = cache_args(), token_args()
+    assert lib.kv_cache_write_dint4(P16, LD, P16, LD, 9, c, t, Z) == b.ERR_DTYPE
+    assert lib.kv_cache_write_dint4(Z, LD, P16, LD, b.F16, c, t, Z) == lib.kv_cache_write_dint4(P16, None, P16, LD, b.F16, c, t, Z) == b.ERR_NULL
+    assert lib.kv_cache_write_dint4(P16, LD, P16, LD, b.F16, None, t, Z) == lib.kv_cache_read_dint4(c, None, P16, P16, b.F16, Z) == b.ERR_NULL
+    assert lib.kv_cache_read_dint4(c, t, ctypes.c_void_p(0x1008), P16, b.F16, Z) == b.ERR_SHAPE
+    assert lib.attention_kv_dint4(P16, LD, 9, 8, c, t, 1.0, 64, P16, Z, 0, Z) == b.ERR_DTYPE
+    for heads, max_len in ((0, 64), (6, 64), (8, -1)):
+        assert lib.attention_kv_dint4(P16, LD, b.F16, heads, c, t, 1.0, max_len, P16, Z, 0, Z) == b.ERR_SHAPE
+        assert lib.attention_kv_dint4_workspace_bytes(b.F16, heads, c, t, max_len) == 0
+    assert lib.attention_kv_dint4(P16, LD, b.F16, 8, c, t, 1.0, 64, ctypes.c_void_p(0x1004), Z, 0, Z) == b.ERR_SHAPE
+    for empty in (dict(batch=0), dict(new_tokens=0)):
+        t = token_args(**empty)
+        assert lib.kv_cache_write_dint4(Z, None, Z, None, b.F16, c, t, Z) == b.OK
+        assert lib.kv_cache_read_dint4(c, t, Z, Z, b.F16, Z) == b.OK
+        assert lib.attention_kv_dint4(Z, None, b.F16, 8, c, t, 1.0, 64, Z, Z, 0, Z) == b.OK
+
+
+def test_python_checks():
+    """The binding's own checks, on CPU tensors: they come before any call."""
+    x = torch.zeros((2, 64), dtype=torch.float16)
+    for kw in (dict(w=torch.ones(63).half()), dict(w=torch.ones(64).bfloat16()), dict(s=torch.ones(64).half()), dict(s=torch.ones(32)),
+               dict(residual=torch.zeros(2, 64)), dict(residual=x[:1]), dict(h=x)):
+        with pytest.raises(ValueError):
+            w.rms_norm_act_int8(x, **{**dict(w=torch.ones(64).half()), **kw})
+    cache = w.KVCacheDint4.empty(4, 2, 16, 64, device="cpu")
+    start, count = torch.zeros(3, dtype=torch.int32), torch.ones(3, dtype=torch.int32)
+    table = torch.zeros((3, 2), dtype=torch.int32)
+    k = torch.zeros((3, 1, 2, 64), dtype=torch.float16)
+    good = dict(k=k, v=k, cache=cache, start=start, count=count, table=table)
+    for kw in (dict(k=k[..., :32]), dict(k=k.float()), dict(v=k[:2]), dict(k=k[:, :, :1], v=k[:, :, :1]), dict(start=start.long()), dict(start=start[:2]),
+               dict(count=count[:2]), dict(table=table.long()), dict(table=table[:2]), dict(table=table.t().contiguous().t()),
+               dict(cache=cache._replace(k_words=cache.k_words[:2])), dict(cache=cache._replace(v_packed=cache.v_packed.int())),
+               dict(k=k.transpose(2, 3).contiguous().transpose(2, 3))):
+        with pytest.raises(ValueError):
+            w.kv_cache_write_dint4(**{**good, **kw})
+    with pytest.raises(ValueError):
+        w.kv_cache_read_dint4(cache, start, -1, count, table)
+    with pytest.raises(ValueError):
+        w.attention_kv_dint4(k[..., :32], cache, start, count, table)
+    with pytest.raises(ValueError):
+        w.KVCacheDint4.empty(1, 1, 16, 60, device="cpu")
+
+
+def test_definition_is_the_weights_rule(oracle):
+    """With a power-of-two step the 20 bits drop nothing: a row is quantized as a weight row is."""
+    g = torch.Generator().manual_seed(3)
+    x = (torch.randn((40, 64), generator=g) * 4).round() / 8
+    x[:, 0], x[:, 1] = -2.5, 4.0              # a range of 13 / 2
+    x = x.clamp(-2.5, 4.0)
+    codes, step, zero = oracle.quantize_weight_dint4(x.numpy(), None, 0)
+    packed, words = du.quantize64(x.half())
+    np.testing.assert_array_equal((words & -16).view(torch.float32).numpy(), step[:, 0])
+    np.testing.assert_array_equal((words & 15).numpy(), zero[:, 0])
+    c = codes.astype(np.int64)
+    ref = np.where(c == 14, 1, np.where(c == 15, -1, 2 * (c - zero.astype(np.int64)))) * (step / 2.0)
+    np.testing.assert_array_equal(du.values64(packed, words).numpy(), ref)

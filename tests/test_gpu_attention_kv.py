@@ -1,0 +1,224 @@
+"""Attention over the 4-bit cache against the definition in float64, at the sizes, masks and places where it can go wrong."""
+import math
+
+import pytest
+import torch
+
+import decoder_util as du
+import paper_2311_05161_amd as w
+from decoder_util import TORCH_DT
+
+pytestmark = pytest.mark.gpu
+
+
+def setup(B, S, Hq, H, D, T, P, dtype, seed=0, spread=1.0, q_gain=1.0):
+    g = torch.Generator().manual_seed(1000 * D + T + S + seed)
+    each = (T + P - 1) // P
+    pages = B * each + 2
+    cache = du.random_cache(g, pages, H, P, D, spread)
+    table = du.random_tables(g, B, each, pages)
+    q = (torch.randn((B, S, Hq, D), generator=g) * q_gain).to(TORCH_DT[dtype])
+    return q, cache, table
+
+
+def run(q, cache, start, count, table, **kw):
+    dev = w.KVCacheDint4(*(t.cuda() for t in cache))
+    ints = [None if x is None else torch.tensor(x, dtype=torch.int32).cuda() for x in (start, count)]
+    return w.attention_kv_dint4(q.cuda(), dev, *ints, table.cuda(), **kw)
+
+
+def check(q, cache, start, count, table, where="", **kw):
+    scale = kw.get("scale") or q.shape[-1] ** -0.5
+    got = run(q, cache, start, count, table, **kw)
+    assert got.shape == q.shape and got.dtype == q.dtype
+    ref, slack = du.attention64(q, cache, start, count, table, scale, kw.get("max_len"))
+    du.assert_attention(got, ref, slack, where)
+    return got
+
+
+CASES = [  # B, S, Hq, H, D, page, dtype, start, count
+    # one token, a few, across tiles and pages
+    (1, 1, 1, 1, 64, 16, "f16", [0], None),
+    (1, 1, 2, 2, 128, 16, "bf16", [1], None),
+    (3, 1, 4, 4, 128, 16, "f16", [14, 15, 16], None),
+    (4, 1, 8, 2, 128, 16, "bf16", [62, 63, 64, 65], [1, 1, 0, 1]),
+    (2, 1, 6, 3, 96, 16, "f16", [599, 130], None),
+    (2, 1, 8, 1, 64, 64, "bf16", [1000, 777], None),
+    (1, 1, 16, 2, 256, 16, "f16", [300], None),
+    (1, 1, 4, 4, 128, 4096, "f16", [4000], None),
+    (2, 1, 5, 1, 128, 16, "f16", [2050, 255], None),
+    (1, 1, 64, 2, 64, 16, "bf16", [513], None),
+    # drafts
+    (2, 2, 4, 4, 128, 16, "f16", [0, 77], None),
+    (3, 5, 6, 3, 64, 16, "f16", [0, 251, 16], [5, 3, 0]),
+    (2, 8, 16, 2, 128, 128, "bf16", [130, 500], [8, 7]),
+    (1, 3, 9, 3, 96, 16, "bf16", [61], None),
+    (2, 8, 4, 2, 256, 64, "bf16", [64, 100], [8, 1]),
+    # prompts and chunks of them
+    (1, 16, 2, 2, 64, 16, "f16", [0], None),
+    (2, 17, 4, 2, 128, 16, "bf16", [0, 100], [17, 9]),
+    (1, 130, 2, 1, 128, 64, "f16", [0], None),
+    (2, 200, 3, 3, 96, 16, "bf16", [0, 333], [200, 131]),
+    (1, 257, 8, 1, 64, 16, "f16", [50], None),
+    (1, 100, 2, 2, 256, 16, "f16", [29], None),
+    (2, 384, 4, 4, 128, 16, "bf16", [0, 0], [384, 1]),
+    (1, 65, 1, 1, 256, 128, "bf16", [700], None),
+    # head sizes, page sizes and types off the usual ones
+    (2, 3, 4, 2, 8, 16, "f16", [0, 40], None),
+    (1, 9, 2, 1, 80, 16, "bf16", [30], None),
+    (2, 2, 2, 2, 512, 16, "f16", [5, 77], None),
+    (2, 4, 4, 2, 128, 1, "f16", [9, 33], [4, 2]),
+    (1, 40, 4, 2, 64, 24, "bf16", [31], None),
+    (1, 20, 2, 2, 128, 7, "f16", [100], None),
+    (2, 5, 4, 2, 128, 16, "f32", [0, 200], [5, 4]),
+    (1, 33, 2, 1, 64, 16, "f32", [64], None),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=[f"{c[0]}x{c[1]}x{c[2]}-{c[3]}x{c[4]}p{c[5]}{c[6]}t{max(c[7])}" for c in CASES])
+def test_against_the_definition(case):
+    B, S, Hq, H, D, P, dtype, start, count = case
+    T = max(start) + S
+    q, cache, table = setup(B, S, Hq, H, D, T, P, dtype)
+    out = check(q, cache, start, count, table)
+    check(q, cache, start, count, table, where="max_len", max_len=T)
+    for b in range(B):
+        c = S if count is None else count[b]
+        assert (out[b, c:] == 0).all()
+
+
+@pytest.mark.parametrize("S,G,D", [(1, 1, 128), (1, 8, 64), (5, 2, 128), (40, 2, 128), (150, 1, 64)])
+def test_what_lies_behind_a_sequence_is_not_looked_at(S, G, D):
+    """Steps that are NaN and infinite, and every page behind the tokens: no output bit changes."""
+    B, H, P, start = 2, 2, 16, [70, 101]
+    q, cache, table = setup(B, S, G * H, H, D, 160 + S, P, "f16")
+    ref = check(q, cache, start, None, table)
+    bad = [t.clone() for t in cache]
+    for b in range(B):
+        for p in range(start[b] + S, table.shape[1] * P):
+            bad[1][table[b, p // P].long(), :, p % P] = 0x7FC00003 if p % 2 else 0x7F800000
+            bad[3][table[b, p // P].long(), :, p % P] = 0x7FC00000 if p % 3 else -0x00800000 + 5
+            bad[0][table[b, p // P].long(), :, p % P] = 0xFF
+    unused = set(range(cache[0].shape[0])) - set(table.flatten().tolist())
+    for n in unused:
+        bad[1][n], bad[3][n] = 0x7FC00000, 0x7FC00000
+    table2 = table.clone()
+    for b in range(B):
+        table2[b, (start[b] + S + P - 1) // P:] = 1 << 30
+    assert torch.equal(run(q, bad, start, None, table2).view(torch.int16), ref.view(torch.int16))
+    assert torch.equal(run(q, bad, start, None, table2, max_len=max(start) + S).view(torch.int16), ref.view(torch.int16))
+
+
+@pytest.mark.parametrize("S,G,D", [(1, 1, 128), (1, 4, 64), (3, 2, 96), (70, 2, 128)])
+def test_pages_that_the_cache_has_not_and_limits(S, G, D):
+    B, H, P, start = 3, 2, 16, [100, 40, 64]
+    q, cache, table = setup(B, S, G * H, H, D, 100 + S, P, "bf16")
+    table[0, 2], table[0, 5], table[1, :] = -1, cache[0].shape[0], -3     # the second sequence sees nothing
+    out = check(q, cache, start, None, table)
+    assert (out[1] == 0).all()
+    for max_len in (0, 1, 33, 90):
+        check(q, cache, start, None, table, where=f"max_len {max_len}", max_len=max_len)
+    check(q, cache, [-4, 5000, 20], [S, S, 99], table, where="clamped")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("S,Hq,H,D", [(1, 2, 2, 128), (2, 8, 1, 64), (64, 2, 1, 128)])
+def test_sharp_and_flat_softmax(S, Hq, H, D, dtype):
+    """Scores of hundreds, equal scores, steps that differ by 2^20, a sink at the first token."""
+    T, P = 700, 16
+    start = [T - S]
+    for gain, spread, scale in ((40.0, 1.0, None), (1e-4, 1.0, None), (1.0, 5.0, 0.01), (1.0, 1.0, -0.3), (0.0, 1.0, None)):
+        q, cache, table = setup(1, S, Hq, H, D, T, P, dtype, spread=spread, q_gain=gain)
+        check(q, cache, start, None, table, where=f"{gain} {spread}", scale=scale or D ** -0.5)
+    q, cache, table = setup(1, S, Hq, H, D, T, P, dtype)
+    cache[1][table[0, 0].long(), :, 0] = torch.tensor(8.0).view(torch.int32).item()
+    check(q, cache, start, None, table, where="sink")
+    zero = [t.clone() for t in cache]
+    zero[1] &= 15                                        # all Keys zero: the mean of the Values
+    check(q, zero, start, None, table, where="zero Keys")
+    zero[3] &= 15
+    assert (run(q, zero, start, None, table) == 0).all()
+
+
+@pytest.mark.parametrize("Hq,H,D,P,T", [(2, 1, 128, 16, 20001), (8, 1, 64, 64, 9000), (1, 1, 128, 40000, 33333)])
+def test_one_long_sequence(Hq, H, D, P, T):
+    q, cache, table = setup(1, 1, Hq, H, D, T, P, "f16")
+    check(q, cache, [T - 1], None, table)
+    check(q, cache, [T - 1], None, table, max_len=T)
+
+
+def test_a_cache_past_32_bits():
+    """Rows further than 2^31 bytes and 2^32 channels from the cache's beginning."""
+    H, P, D, pages = 8, 64, 128, 70000
+    cache = w.KVCacheDint4.empty(pages, H, P, D)
+    for t in cache:
+        t.zero_()
+    far = torch.tensor([[69999, 35000, 66000, 3]], dtype=torch.int32)
+    g = torch.Generator().manual_seed(4)
+    for S in (1, 40):
+        k, v = (torch.randn((1, 200, H, D), generator=g).half().cuda() for _ in range(2))
+        start = torch.zeros(1, dtype=torch.int32).cuda()
+        w.kv_cache_write_dint4(k, v, cache, start, None, far.cuda())
+        small = w.KVCacheDint4.empty(4, H, P, D)
+        near = torch.tensor([[1, 0, 3, 2]], dtype=torch.int32).cuda()
+        w.kv_cache_write_dint4(k, v, small, start, None, near)
+        for a, b in zip(w.kv_cache_read_dint4(cache, start, 200, None, far.cuda()), w.kv_cache_read_dint4(small, start, 200, None, near)):
+            assert torch.equal(a, b)
+        q = torch.randn((1, S, 16, D), generator=g).half().cuda()
+        at = torch.tensor([200 - S], dtype=torch.int32).cuda()
+        assert torch.equal(w.attention_kv_dint4(q, cache, at, None, far.cuda()), w.attention_kv_dint4(q, small, at, None, near))
+
+
+@pytest.mark.parametrize("S,G,D", [(1, 1, 128), (4, 4, 64), (100, 2, 128)])
+def test_strides_forms_streams_graphs(S, G, D, monkeypatch):
+    B, H, P, start = 2, 2, 16, [50, 333]
+    q, cache, table = setup(B, S, G * H, H, D, 333 + S, P, "f16")
+    ref = check(q, cache, start, None, table)
+    dev = w.KVCacheDint4(*(t.cuda() for t in cache))
+    st, tb = torch.tensor(start, dtype=torch.int32).cuda(), table.cuda()
+    for pad in (0, 8, 3):                                # cut out of a fused projection's output
+        fused = torch.zeros((B, S, (G + 2) * H * D + pad), dtype=torch.float16, device="cuda")
+        qv = fused[..., pad:pad + G * H * D].unflatten(-1, (G * H, D))
+        qv.copy_(q)
+        assert torch.equal(w.attention_kv_dint4(qv, dev, st, None, tb), ref)
+    wide = torch.full((B, table.shape[1] + 5), -1, dtype=torch.int32, device="cuda")
+    wide[:, :-5] = tb
+    assert torch.equal(w.attention_kv_dint4(q.cuda(), dev, st, None, wide[:, :-5]), ref)
+    qd = q.cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = w.attention_kv_dint4(qd.clone(), dev, st, None, tb)
+    side.synchronize()
+    assert torch.equal(other, ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        other = w.attention_kv_dint4(qd, dev, st, None, tb, max_len=333 + S)
+    eager = w.attention_kv_dint4(qd, dev, st, None, tb, max_len=333 + S)
+    for _ in range(3):
+        other.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(other, eager)
+    st -= 20                                             # the lengths are read when the graph runs
+    graph.replay()
+    torch.cuda.synchronize()
+    r, slack = du.attention64(q, cache, [s - 20 for s in start], None, table, 1 / math.sqrt(D))
+    du.assert_attention(other, r, slack)
+    st += 20
+    monkeypatch.setattr(w.binding, "_native", False)
+    assert torch.equal(w.attention_kv_dint4(qd, dev, st, None, tb), ref)
+    empty = w.attention_kv_dint4(qd[:, :0], dev, st, None, tb)
+    assert empty.shape == (B, 0, G * H, D)
+
+
+def test_refusals():
+    q, cache, table = setup(1, 1, 4, 2, 64, 32, 16, "f16")
+    with pytest.raises(w.W4A8Error):
+        run(q[:, :, :3], cache, [5], None, table)
+    with pytest.raises(w.W4A8Error):
+        run(q, cache, [5], None, table, max_len=-1)
+    with pytest.raises(ValueError):
+        run(q[..., :32], cache, [5], None, table)
+    with pytest.raises(KeyError):
+        run(q.double(), cache, [5], None, table)

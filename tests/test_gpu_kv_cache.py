@@ -1,0 +1,190 @@
+"""The 4-bit cache: written rows bit for bit against the rule in exact arithmetic, what is read back to one rounding."""
+import pytest
+import torch
+
+import decoder_util as du
+import paper_2311_05161_amd as w
+from decoder_util import TORCH_DT
+
+pytestmark = pytest.mark.gpu
+
+
+def rows(g, B, S, H, D, dtype):
+    x = torch.randn((B, S, H, D), generator=g) * torch.exp2(torch.randn((H, D), generator=g))
+    x[..., :2] *= 4.0
+    x[:, ::3, 0] = 0.0                                   # rows of zeros
+    if S > 1:
+        x[:, 1] = x[:, 1].abs()                          # zero-point 0
+        x[:, 1, -1] = -x[:, 1, -1]                       # .. 13
+    return x.to(dtype)
+
+
+def fresh(pages, H, P, D):
+    """Pages that hold a pattern, to see what is not written."""
+    return w.KVCacheDint4(*(torch.full((pages, H, P, D // 2), 0xA5, dtype=torch.uint8, device="cuda") if i % 2 == 0 else
+                            torch.full((pages, H, P), -7, dtype=torch.int32, device="cuda") for i in range(4)))
+
+
+CASES = [  # B, S, H, D, page, dtype, start, count
+    (1, 1, 1, 8, 1, "f16", [0], None),
+    (3, 1, 5, 64, 16, "bf16", [0, 7, 31], None),
+    (2, 7, 3, 128, 16, "f16", [0, 13], [7, 4]),
+    (2, 5, 4, 96, 16, "bf16", [3, 30], [5, 0]),
+    (1, 33, 2, 256, 24, "f16", [5], [33]),
+    (4, 2, 40, 128, 64, "bf16", [0, 1, 63, 64], [2, 1, 2, 2]),
+    (2, 9, 2, 512, 5, "f16", [0, 11], [9, 9]),
+    (2, 6, 3, 80, 16, "bf16", [1, 2], [6, 3]),
+    (1, 300, 2, 64, 128, "f16", [90], [290]),
+    (2, 16, 1, 264, 16, "bf16", [0, 15], None),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=[f"{c[0]}x{c[1]}x{c[2]}x{c[3]}p{c[4]}{c[5]}" for c in CASES])
+def test_write_and_read(case):
+    B, S, H, D, P, dtype, start, count = case
+    g = torch.Generator().manual_seed(S + D)
+    k, v = rows(g, B, S, H, D, TORCH_DT[dtype]), rows(g, B, S, H, D, TORCH_DT[dtype])
+    each = (max(start) + S + P - 1) // P
+    pages = B * each + 3
+    table = du.random_tables(g, B, each, pages)
+    cache = fresh(pages, H, P, D)
+    st, ct = torch.tensor(start, dtype=torch.int32).cuda(), None if count is None else torch.tensor(count, dtype=torch.int32).cuda()
+    w.kv_cache_write_dint4(k.cuda(), v.cuda(), cache, st, ct, table.cuda())
+    want = [t.cpu() for t in fresh(pages, H, P, D)]
+    for n, x in ((0, k), (2, v)):
+        packed, words = du.quantize64(x)
+        for b in range(B):
+            for i in range(S if count is None else count[b]):
+                p = start[b] + i
+                want[n][table[b, p // P].long(), :, p % P] = packed[b, i]
+                want[n + 1][table[b, p // P].long(), :, p % P] = words[b, i]
+    for got, ref, what in zip(cache, want, ("k_packed", "k_words", "v_packed", "v_words")):
+        assert torch.equal(got.cpu(), ref), f"{what}: {int((got.cpu() != ref).sum())} differ"
+    for out in (torch.float32, torch.float16, torch.bfloat16):
+        gk, gv = w.kv_cache_read_dint4(cache, st, S, ct, table.cuda(), dtype=out)
+        for got, n in ((gk, 0), (gv, 2)):
+            assert got.shape == (B, S, H, D) and got.dtype == out
+            for b in range(B):
+                c = S if count is None else count[b]
+                assert (got[b, c:] == 0).all()
+                pos = start[b] + torch.arange(c)
+                ref = du.values64(want[n][table[b][pos // P].long(), :, pos % P], want[n + 1][table[b][pos // P].long(), :, pos % P])
+                # (25-bit products are rounded to binary32 before they are rounded to 16 bits)
+                assert torch.equal(got[b, :c].cpu(), ref.float().to(out))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_borders_are_decided_exactly(dtype):
+    """Rows whose values lie on the borders of the rule: ranges of 13 times many steps, with x = step times 1/4, 1/2, 3/4, 3/2 ..."""
+    dt = TORCH_DT[dtype]
+    D, out = 64, []
+    for m in range(1, 256):
+        for z in (0, 3, 6, 13):
+            step = m * 2.0 ** -6
+            u = torch.cat([torch.arange(-z * 4, (13 - z) * 4 + 1) * 0.25, torch.tensor([-float(z), 13.0 - z])])
+            x = torch.zeros(D, dtype=torch.float64)
+            x[: len(u)] = u * step
+            out.append(x)
+    for m in range(1, 129):                              # -lo = hi: the zero-point's own tie
+        out.append(torch.linspace(-m, m, D, dtype=torch.float64))
+    x = torch.stack(out).to(dt).reshape(1, -1, 1, D)
+    S = x.shape[1]
+    cache = w.KVCacheDint4.empty(1, 1, S, D)
+    start, table = torch.zeros(1, dtype=torch.int32).cuda(), torch.zeros((1, 1), dtype=torch.int32).cuda()
+    w.kv_cache_write_dint4(x.cuda(), x.cuda(), cache, start, None, table)
+    packed, words = du.quantize64(x[0, :, 0])
+    assert torch.equal(cache.k_words[0, 0].cpu(), words) and torch.equal(cache.v_packed[0, 0].cpu(), packed)
+
+
+def test_binary32_rows():
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn((2, 40, 3, 128), generator=g) * 3
+    x[0, 0] *= 1e30
+    x[0, 1] *= 1e-30
+    x[0, 2] *= 1e-39                                     # a step below the normal range: zeros
+    cache = w.KVCacheDint4.empty(6, 3, 16, 128)
+    start, table = torch.zeros(2, dtype=torch.int32).cuda(), torch.arange(6, dtype=torch.int32).reshape(2, 3).cuda()
+    w.kv_cache_write_dint4(x.cuda(), x.cuda(), cache, start, None, table)
+    k, v = w.kv_cache_read_dint4(cache, start, 40, None, table, dtype=torch.float32)
+    assert torch.equal(k, v)
+    xd = x.double()
+    step = du.round_step((xd.amax(-1).clamp(min=0) - xd.amin(-1).clamp(max=0)) / 13)
+    # half a step, the ends' (13 steps of 20 bits, a zero-point half a step off) one step, the quotient's 2^-20
+    inside = ((xd / step[..., None]).abs() < 0.75)
+    err = (k.cpu().double() - xd).abs()
+    assert (k.cpu()[0, 2] == 0).all()
+    live = step > 0
+    assert (err <= (1.0 + 2.0 ** -15) * step[..., None])[live].all()
+    assert (err <= (0.25 + 2.0 ** -15) * step[..., None])[live][inside[live]].all()
+    packed, words = du.quantize64(xd)
+    assert (k.cpu().double() == du.values64(packed, words)).double().mean() > 0.999
+
+
+def test_strides_streams_and_forms(monkeypatch):
+    """Rows cut out of a fused projection's output, at any alignment; the Python form; another stream; a graph."""
+    B, S, H, D, P = 2, 20, 4, 64, 16
+    g = torch.Generator().manual_seed(11)
+    k, v = rows(g, B, S, H, D, torch.float16), rows(g, B, S, H, D, torch.float16)
+    table = du.random_tables(g, B, 3, 8).cuda()
+    start, count = torch.tensor([3, 0], dtype=torch.int32).cuda(), torch.tensor([20, 11], dtype=torch.int32).cuda()
+    ref = fresh(8, H, P, D)
+    w.kv_cache_write_dint4(k.cuda(), v.cuda(), ref, start, count, table)
+    for pad in (0, 8, 1):
+        fused = torch.zeros((B, S, 3 * H * D + pad), dtype=torch.float16, device="cuda")
+        kv, vv = (fused[..., pad + i * H * D:pad + (i + 1) * H * D].unflatten(-1, (H, D)) for i in (1, 2))
+        kv.copy_(k), vv.copy_(v)
+        got = fresh(8, H, P, D)
+        w.kv_cache_write_dint4(kv, vv, got, start, count, table)
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    got = fresh(8, H, P, D)
+    w.kv_cache_write_dint4(k.transpose(1, 2).contiguous().transpose(1, 2).cuda(), v.cuda(), got, start, count, table)
+    assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    values = w.kv_cache_read_dint4(ref, start, S, count, table)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        got = fresh(8, H, P, D)
+        w.kv_cache_write_dint4(k.cuda(), v.cuda(), got, start, count, table)
+        other = w.kv_cache_read_dint4(got, start, S, count, table)
+    st.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(other, values))
+    kd, vd, got = k.cuda(), v.cuda(), fresh(8, H, P, D)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w.kv_cache_write_dint4(kd, vd, got, start, count, table)
+        other = w.kv_cache_read_dint4(got, start, S, count, table)
+    for _ in range(3):
+        [t.zero_() for t in (*got, *other)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(other, values))
+    monkeypatch.setattr(w.binding, "_native", False)
+    got = fresh(8, H, P, D)
+    w.kv_cache_write_dint4(kd, vd, got, start, count, table)
+    assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    assert all(torch.equal(a, b) for a, b in zip(w.kv_cache_read_dint4(got, start, S, count, table), values))
+
+
+def test_places_that_are_not_there():
+    """Pages that the cache has not, starts and counts out of range: nothing is written or read out of place."""
+    B, S, H, D, P = 5, 6, 2, 64, 4
+    g = torch.Generator().manual_seed(2)
+    k = rows(g, B, S, H, D, torch.float16).cuda()
+    table = torch.tensor([[0, -1, 1], [2, 10, 3], [4, 5, 6], [7, 8, 9], [8, 8, 8]], dtype=torch.int32)   # of 10 pages
+    start = torch.tensor([1, 2, -5, 10, 400], dtype=torch.int32)     # the fourth is cut at 12 positions, the last has no room
+    count = torch.tensor([6, 6, 2, 50, 6], dtype=torch.int32)
+    cache = fresh(10, H, P, D)
+    w.kv_cache_write_dint4(k, k, cache, start.cuda(), count.cuda(), table.cuda())
+    packed, words = du.quantize64(k.cpu())
+    want = [t.cpu() for t in fresh(10, H, P, D)]
+    seen = torch.zeros((B, S), dtype=torch.bool)
+    for b, (s0, c) in enumerate(zip([1, 2, 0, 10, 12], [6, 6, 2, 2, 0])):
+        for i in range(c):
+            page = int(table[b, (s0 + i) // P])
+            if 0 <= page < 10:
+                seen[b, i] = True
+                for n in (0, 2):
+                    want[n][page, :, (s0 + i) % P], want[n + 1][page, :, (s0 + i) % P] = packed[b, i], words[b, i]
+    assert all(torch.equal(a.cpu(), r) for a, r in zip(cache, want))
+    got = w.kv_cache_read_dint4(cache, start.cuda(), S, count.cuda(), table.cuda(), dtype=torch.float32)[0].cpu()
+    assert torch.equal(got, torch.where(seen[..., None, None], du.values64(packed, words).float(), 0.0))
