@@ -222,9 +222,8 @@ def _run_norm(st):
     x, r, w, s = st["x"], st["r"], st["w"], st["s"]
     if own:
         import paper_2311_05161_amd as lib
-        q, sx, h = lib.rms_norm_act_int8(x, w, eps=st["eps"], residual=r, s=s)
-        y = torch.mul(q, sx[:, None], out=torch.empty_like(x))
-        return (y, sx, h) if r is not None else (y, sx)
+        q, sx, *h = lib.rms_norm_act_int8(x, w, eps=st["eps"], residual=r, s=s)
+        return (torch.mul(q, sx[:, None], out=torch.empty_like(x)), sx, *h)
     h = x if r is None else (x.float() + r.float()).to(x.dtype)
     f = h.float()
     gain = w.float() if s is None else w.float() * (1.0 / s)
