@@ -410,7 +410,8 @@ int rms_norm_act_int8(const void *X, int x_dtype, int64_t M, int64_t K, int64_t 
  * (F16 and BF16 rows: as in exact arithmetic, ties and borders included).  Its head_dim / 2 bytes are the tiled layout's words
  * in a row (word q: channels 8q .. 8q+7, see W4A8_LAYOUT_TILED), its word the bits of the step with z in the last four.
  *   k_packed, v_packed   [pages, heads, page_size, head_dim / 2] bytes      k_words, v_words   [pages, heads, page_size] int32
- * All four 16-byte aligned; head_dim a multiple of 8, 8 .. 512; page_size >= 1.
+ * The page_size rows of a (page, head) are contiguous; where the next head's and the next page's begin is free (page_ld, head_ld;
+ * heads * page_size and page_size for a dense cache), the same for all four.  All four 16-byte aligned; head_dim a multiple of 8, 8 .. 512; page_size >= 1.
  * (The struct is read on the host; its pointers are device pointers.) */
 typedef struct {
     uint8_t *k_packed;
@@ -418,6 +419,7 @@ typedef struct {
     uint8_t *v_packed;
     int32_t *v_words;
     int64_t pages, heads, page_size, head_dim;
+    int64_t page_ld, head_ld;   /* distances between pages and between the heads of a page, in rows */
 } w4a8_kv_cache;
 
 /* Where the tokens of one step are.  Sequence b has start[b] cached tokens before the step and count[b] <= new_tokens new ones

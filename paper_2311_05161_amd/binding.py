@@ -53,7 +53,7 @@ _addr = {}       # the addresses of the entry points that it calls (replaced as 
 
 class _KVCacheArgs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("k_packed", "k_words", "v_packed", "v_words")] + \
-               [(n, ctypes.c_int64) for n in ("pages", "heads", "page_size", "head_dim")]
+               [(n, ctypes.c_int64) for n in ("pages", "heads", "page_size", "head_dim", "page_ld", "head_ld")]
 
 
 class _KVTokensArgs(ctypes.Structure):
@@ -702,7 +702,8 @@ def rms_norm_act_int8(x: torch.Tensor, w: torch.Tensor, eps: float = 1e-5, resid
 
 class KVCacheDint4(typing.NamedTuple):
     """The 4-bit cache of Keys and Values of a layer: packed uint8 [pages, heads, page_size, head_dim / 2], words int32
-    [pages, heads, page_size], both for Keys and for Values."""
+    [pages, heads, page_size], both for Keys and for Values.  The rows of a page and head are contiguous; pages and heads may
+    lie in another order (a [heads, pages, ..] cache seen through transpose(0, 1)), the same in all four."""
     k_packed: torch.Tensor
     k_words: torch.Tensor
     v_packed: torch.Tensor
@@ -722,10 +723,19 @@ def _kv_args(cache, start, count, table):
     kp = cache.k_packed
     if kp.dim() != 4:
         raise ValueError("packed rows must be [pages, heads, page_size, head_dim / 2]")
+    ld = []
     for t, want, dtype in ((cache.k_packed, kp.shape, torch.uint8), (cache.k_words, kp.shape[:3], torch.int32),
                            (cache.v_packed, kp.shape, torch.uint8), (cache.v_words, kp.shape[:3], torch.int32)):
-        if t.shape != want or t.dtype != dtype or not t.is_contiguous() or t.device != kp.device:
-            raise ValueError("the cache's tensors must be contiguous, of one device and one set of pages: uint8 rows, int32 words")
+        if t.shape != want or t.dtype != dtype or t.device != kp.device:
+            raise ValueError("the cache's tensors must be of one device and one set of pages: uint8 rows, int32 words")
+        # rows contiguous in a (page, head), and as far apart in all four (a dimension of one has no distance)
+        row = kp.shape[3] if t.dim() == 4 else 1
+        page, head = (t.stride(i) if t.shape[i] > 1 else 0 for i in range(2))
+        if row < 1 or (t.dim() == 4 and row > 1 and t.stride(3) != 1) or (t.shape[2] > 1 and t.stride(2) != row) or page % row or head % row:
+            raise ValueError("the rows of a page and head must be contiguous in the cache's tensors")
+        ld.append((page // row, head // row))
+    if len(set(ld)) > 1:
+        raise ValueError("pages and heads must be as far apart in all four of the cache's tensors")
     if start.dim() != 1:
         raise ValueError("start must be a vector, one number for each sequence")
     B = start.shape[0]
@@ -737,7 +747,7 @@ def _kv_args(cache, start, count, table):
         raise ValueError("table must be int32 [sequences, pages] with contiguous rows, on the cache's device")
     pages, heads, page_size, half = kp.shape
     c = _KVCacheArgs(kp.data_ptr(), cache.k_words.data_ptr(), cache.v_packed.data_ptr(), cache.v_words.data_ptr(), pages, heads,
-                     page_size, 2 * half)
+                     page_size, 2 * half, *ld[0])
     t = _KVTokensArgs(start.data_ptr(), None if count is None else count.data_ptr(), table.data_ptr(),
                       table.stride(0) if B > 1 else max(table.stride(0), table.shape[1]), table.shape[1], B, 0)
     return c, t

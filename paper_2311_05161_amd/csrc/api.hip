@@ -211,7 +211,7 @@ static int kv_shape(const w4a8_kv_cache *c, const w4a8_kv_tokens *t)
 {
     if (!c || !t) return W4A8_ERR_NULL;
     if (c->pages < 0 || c->heads < 1 || c->heads > 65535 || c->page_size < 1 || c->page_size > 0x7fffffffLL) return W4A8_ERR_SHAPE;
-    if (c->head_dim < 8 || c->head_dim > 512 || c->head_dim % 8 != 0 || c->pages > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+    if (c->head_dim < 8 || c->head_dim > 512 || c->head_dim % 8 != 0 || c->pages > 0x7fffffffLL || c->page_ld < 0 || c->head_ld < 0) return W4A8_ERR_SHAPE;
     if (t->batch < 0 || t->batch > 0x7fffffffLL || t->new_tokens < 0 || t->table_pages < 0 || t->table_ld < t->table_pages) return W4A8_ERR_SHAPE;
     // (positions are numbered in 32 bits, and the step's tokens are part of them)
     if (t->table_pages > 0x7fffffffLL / c->page_size || t->new_tokens > 0x7fffffffLL) return W4A8_ERR_SHAPE;
@@ -228,7 +228,7 @@ static int kv_pointers(const w4a8_kv_cache *c, const w4a8_kv_tokens *t)
 }
 static KvView kv_view(const w4a8_kv_cache *c)
 {
-    return {{c->k_packed, c->v_packed}, {c->k_words, c->v_words}, c->pages, (int)c->heads, (int)c->page_size, (int)c->head_dim};
+    return {{c->k_packed, c->v_packed}, {c->k_words, c->v_words}, c->pages, c->page_ld, c->head_ld, (int)c->heads, (int)c->page_size, (int)c->head_dim};
 }
 static KvTokens kv_tokens(const w4a8_kv_tokens *t)
 {

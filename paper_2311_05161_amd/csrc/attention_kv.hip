@@ -3,6 +3,8 @@
 //     o[b, i, h] = sum_t p_t v_t,   p = softmax_t(scale q[b, i, h] . k_t),   t = 0 .. start[b] + i
 //
 // with the h / (Hq / Hkv)-th head of the cache.  A query that is not there (i >= count[b]) gives zeros.
+#include <algorithm>
+
 #include "kv_dint4.hpp"
 
 namespace w4a8 {
@@ -83,6 +85,515 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs p, KvView c, Kv
     }
 }
 
+// ---- few query rows per head of the cache: the cache streams once through registers --------------------------------------------
+//
+// The cache's levels go to the 16-bit matrix cores as small whole numbers, exactly: with the step worth 16 units,
+//     n = level / (step / 16) + 16 z + 8:   16 c + 8 for the codes c = 0..13,   16 z and 16 z + 16 for -+step/2
+// are bytes 0..224, and a byte with a zero above it IS the fp16 number n 2^-24 (a subnormal; the matrix cores take them as
+// they are, checked on this card).  So a nibble costs a table look-up in a register (its base level by a byte permute, its
+// upper bit added) and half a permute that spreads bytes to halves.  For Keys 16 z + 8 comes off each score with the sum of q; for
+// Values it is taken off before the product (one packed subtraction for two): a token with nearly all of the weight would otherwise
+// leave 2^-20 of 16 z + 8 in channels that are zero.  Queries enter as fp16 as they are (bf16: times a power of two per row, so that nothing is lost); the softmax's weights
+// enter as fp16 numbers p step 2^(12 - E), E the exponent of the largest step so far: their rounding to 11 bits is the only one on
+// the way, 2^26 below the largest p step they still have all of them, and 2^37 below it they end.
+//
+// A wave takes 64 tokens at a time, alone: scores as (16 tokens) x (16 rows) tiles leave in each lane four tokens of one
+// row, which is what the product with the Values (tokens as the inner dimension, 16 channels x 16 rows out) wants as its
+// operand, so nothing moves between lanes.  With at most 8 (4) rows the 16 columns hold them twice (four times), and each copy
+// does the softmax of another block of 16 tokens.  The running maximum moves only when a score passes it by 2^2.
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+struct StreamArgs {
+    AttnArgs a;
+    float *part_o, *part_ml;   // more than one split: [B][heads][rows][splits][D], [..][2] (maximum and sum)
+    int rows, row_tiles, splits, chunk;
+    int page_jump, page_rest;  // a wave's next tile is this many pages and tokens on
+    int q_vec;                 // queries can be loaded 16 bytes at a time
+};
+
+constexpr float KV_NONE = -1e30f;      // the maximum of no scores
+constexpr float KV_MASKED = -3e38f;
+constexpr float KV_SLACK = 2.0f;       // log2 of what a p may pass the running maximum by
+
+__device__ __forceinline__ uint32_t kv_lut_hi(int32_t word) { return ((uint32_t)word << 28) | 0x00C8A888u; }
+constexpr uint32_t KV_LUT_LO = 0x68482808u;
+// four nibbles (the low ones of p's bytes) -> four bytes n
+__device__ __forceinline__ uint32_t kv_bytes(uint32_t p, uint32_t hi)
+{
+    return __builtin_amdgcn_perm(hi, KV_LUT_LO, p & 0x07070707u) + ((p & 0x08080808u) << 1);
+}
+
+template <typename T> __device__ __forceinline__ void load_q8(const T *p, bool vec, float (&v)[8])
+{
+    if (vec) {
+        const v4u w = *reinterpret_cast<const v4u *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint16_t lo = (uint16_t)(w[i] & 0xffffu), hi = (uint16_t)(w[i] >> 16);
+            v[2 * i] = to_f32(__builtin_bit_cast(T, lo));
+            v[2 * i + 1] = to_f32(__builtin_bit_cast(T, hi));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_f32(p[i]);
+    }
+}
+
+// the power of two (as a float) that brings a row of magnitude `top` to 2^14 .. 2^15; 1 for fp16, whose rows fit as they are
+template <typename T> __device__ __forceinline__ float q_power(float top);
+template <> __device__ __forceinline__ float q_power<__half>(float) { return 1.0f; }
+template <> __device__ __forceinline__ float q_power<bf16_t>(float top)
+{
+    const int e = min(max((int)(__float_as_uint(top) >> 23 & 255u), 15), 254);
+    return __uint_as_float((uint32_t)min(268 - e, 253) << 23);
+}
+
+template <int D> struct StreamShape {
+    static constexpr int W = D / 32;                       // words of a Key row per lane (four lanes to a row)
+    static constexpr int VW = D == 256 ? 2 : 1;            // words of a Value row per lane (16 lanes to a row)
+    static constexpr bool HALVES = D == 64;                // eight words to a row: a lane has one nibble half of one
+    static constexpr int NJ = HALVES ? 4 : 8 * VW;         // channels per lane
+};
+
+template <typename T, int D, int RP, int RT, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, KvView c, KvTokens t)
+{
+    using Shape = StreamShape<D>;
+    constexpr int W = Shape::W, VW = Shape::VW, NJ = Shape::NJ;
+    constexpr int NB = RP / 4;                             // blocks of 16 tokens whose softmax a lane does, of the tile's four
+    constexpr int ROWS = RP * RT;
+    static_assert(RT == 1 || RP == 16, "copies of the rows only where one tile holds them");
+    extern __shared__ float lds[];                         // [NW][ROWS][2], [NW][ROWS][D + 4]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, kg = lane >> 4;
+    int id = blockIdx.x;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int rt = id % p.row_tiles;
+    id /= p.row_tiles;
+    const int h = id % c.heads, b = id / c.heads;
+    const int group = p.a.group, row0 = rt * ROWS;
+    const KvLength len = kv_length(t, c, b);
+
+    // what the rows see: lim_lo .. lim_hi tokens
+    const int s_lo = row0 / group, s_hi = min((min(p.rows, row0 + ROWS) - 1) / group, len.count - 1);
+    const bool some = s_lo < len.count;
+    const int lim_lo = some ? min(len.start + s_lo + 1, p.a.max_len) : 0;
+    const int lim_hi = some ? min(len.start + s_hi + 1, p.a.max_len) : 0;
+    const int t0 = split * p.chunk, t1 = min(lim_hi, t0 + p.chunk);
+
+    float M[RT], l[RT];
+    v4f acc[RT][NJ];
+    int E = -114;                                          // .. 126
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        M[x] = KV_NONE;
+        l[x] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[x][j] = v4f{0, 0, 0, 0};
+    }
+
+    if (t0 + wave * 64 < t1) {
+        // ---- queries
+        v8h q[RT][W];
+        float rowc[RT], q16[RT], q8[RT];
+        int lim[RT];
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            const int r = min(row0 + x * 16 + (col & (RP - 1)), p.rows - 1), s = r / group;
+            lim[x] = s < len.count ? min(len.start + s + 1, p.a.max_len) : lim_hi;
+            const T *src = (const T *)p.a.q + b * p.a.q_ld_b + s * p.a.q_ld_s + (h * group + (r - s * group)) * p.a.q_ld_h + kg * (D / 4);
+            float f[W][8], top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                load_q8<T>(src + 8 * j, p.q_vec, f[j]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[j][i]));
+            }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float power = q_power<T>(top), turn = p.a.scale_log2 < 0.0f ? -power : power;
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    q[x][j][i] = (_Float16)(f[j][i] * turn);
+                    sum += (float)q[x][j][i];
+                }
+            }
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            q16[x] = -sum * 0x1p-20f;                       // -16 units of every token's zero-point
+            q8[x] = -sum * 0x1p-21f;
+            rowc[x] = fabsf(p.a.scale_log2) * 0x1p20f / power;
+        }
+
+        // ---- the tiles' pages
+        int page_j[4], page_off[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int tok = t0 + wave * 64 + 16 * k;
+            page_j[k] = tok / c.page_size;
+            page_off[k] = tok - page_j[k] * c.page_size;
+        }
+        const int32_t *table = t.table + b * t.table_ld;
+        int32_t page[4];
+        auto ask_pages = [&]() {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) page[k] = table[min(page_j[k], t.table_cols - 1)];
+        };
+        int64_t row[4];
+        uint32_t ok = 0, ok_next = 0;
+        auto place_rows = [&]() {                           // (blocks past the table are past every row's limit too)
+            ok_next = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool good = page[k] >= 0 && page[k] < c.pages;
+                ok_next |= good ? 1u << k : 0u;
+                row[k] = (good ? page[k] * c.page_ld + page_off[k] : 0) + h * c.head_ld;
+                page_j[k] += p.page_jump;
+                page_off[k] += p.page_rest;
+                if (page_off[k] >= c.page_size) {
+                    page_off[k] -= c.page_size;
+                    ++page_j[k];
+                }
+            }
+        };
+
+        // ---- raw rows
+        uint32_t kraw[4][W], vraw[4][4][VW];
+        int32_t kz[4];
+        v4i vw[4], skw[NB], svw[NB];
+        const int sgrp = col / RP;                          // lane's copy of the rows: blocks sgrp, sgrp + 16 / RP, ..
+        auto load_k = [&]() {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[0] + row[k] * (D / 2) + col * (D / 2) + kg * (D / 8));
+#pragma unroll
+                for (int j = 0; j < W; ++j) kraw[k][j] = src[j];
+                kz[k] = (c.words[0] + row[k])[col];
+            }
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                int64_t at = row[n * (4 / NB)];
+#pragma unroll
+                for (int k = 1; k < 4 / NB; ++k) at = sgrp == k ? row[n * (4 / NB) + k] : at;
+                skw[n] = *reinterpret_cast<const v4i *>(c.words[0] + at + 4 * kg);
+            }
+        };
+        auto load_v = [&]() {
+            const int word = Shape::HALVES ? col & 7 : D == 96 ? min(col, 11) : VW * col;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint8_t *src = c.packed[1] + row[k] * (D / 2) + 4 * kg * (D / 2) + 4 * word;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int v = 0; v < VW; ++v) vraw[k][r][v] = reinterpret_cast<const uint32_t *>(src + r * (D / 2))[v];
+                vw[k] = *reinterpret_cast<const v4i *>(c.words[1] + row[k] + 4 * kg);
+            }
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                if (NB == 4) {
+                    svw[n] = vw[n];
+                } else {
+                    int64_t at = row[n * (4 / NB)];
+#pragma unroll
+                    for (int k = 1; k < 4 / NB; ++k) at = sgrp == k ? row[n * (4 / NB) + k] : at;
+                    svw[n] = *reinterpret_cast<const v4i *>(c.words[1] + at + 4 * kg);
+                }
+            }
+        };
+
+        ask_pages();
+        place_rows();
+        load_k();
+        load_v();
+        ask_pages();
+        ok = ok_next;
+
+        for (int tok = t0 + wave * 64; tok < t1; tok += NW * 64) {
+            const bool more = tok + NW * 64 < t1;
+            // ---- scores: y = sum q (level in units) times the step
+            float y[RT][NB][4];
+            {
+                v4f sc[RT][4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) sc[x][k] = v4f{q8[x], q8[x], q8[x], q8[x]};
+                    const uint32_t hi = kv_lut_hi(kz[k]);
+#pragma unroll
+                    for (int j = 0; j < W; ++j) {
+                        const uint32_t lo4 = kv_bytes(kraw[k][j], hi), hi4 = kv_bytes(kraw[k][j] >> 4, hi);
+                        const v4u n = {__builtin_amdgcn_perm(0u, lo4, 0x0c010c00u), __builtin_amdgcn_perm(0u, lo4, 0x0c030c02u),
+                                       __builtin_amdgcn_perm(0u, hi4, 0x0c010c00u), __builtin_amdgcn_perm(0u, hi4, 0x0c030c02u)};
+#pragma unroll
+                        for (int x = 0; x < RT; ++x)
+                            sc[x][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, n), q[x][j], sc[x][k], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < RT; ++x)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            float a = sc[x][n * (4 / NB)][r];
+#pragma unroll
+                            for (int k = 1; k < 4 / NB; ++k) a = sgrp == k ? sc[x][n * (4 / NB) + k][r] : a;
+                            const int32_t w = skw[n][r];
+                            y[x][n][r] = __builtin_fmaf((float)(w & 15), q16[x], a) * __int_as_float(w & -16);
+                        }
+            }
+            const bool whole = ok == 15u && tok + 64 <= lim_lo;
+            if (more) {
+                place_rows();
+                load_k();
+            }
+            // ---- softmax
+            uint32_t live = ~0u;                            // bit 4 n + r of each x in turn
+            if (!whole) {
+                live = 0;
+#pragma unroll
+                for (int x = 0; x < RT; ++x)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int k = n * (4 / NB) + (NB == 4 ? 0 : sgrp);
+                            const bool in = tok + 16 * k + 4 * kg + r < lim[x] && (ok >> k & 1u);
+                            live |= in ? 1u << (x * 16 + 4 * n + r) : 0u;
+                            y[x][n][r] = in ? y[x][n][r] : KV_MASKED;
+                        }
+            }
+            const uint32_t any_row = RT > 1 ? live | live >> 16 : live;
+            uint32_t top_step = 0;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top_step = max(top_step, (any_row >> (4 * n + r) & 1u) ? (uint32_t)svw[n][r] & 0x7fffffffu : 0u);
+            bool move = (int)(top_step >> 23) - 127 > E;
+            float top[RT];
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                top[x] = y[x][0][0];
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) top[x] = fmaxf(top[x], y[x][n][r]);
+                top[x] *= rowc[x];
+                move = move || top[x] > M[x] + KV_SLACK;
+            }
+            if (__builtin_amdgcn_ballot_w64(move)) {        // rare: another maximum, or a larger step
+                uint32_t e = top_step >> 23;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) e = max(e, (uint32_t)__shfl_xor((int)e, d));
+                const int E_new = max(E, (int)e - 127);
+                const float shift = __builtin_ldexpf(1.0f, E - E_new);
+                E = __builtin_amdgcn_readfirstlane(E_new);
+#pragma unroll
+                for (int x = 0; x < RT; ++x) {
+                    float m = fmaxf(top[x], M[x]);
+#pragma unroll
+                    for (int d = RP; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+                    const float keep = __builtin_amdgcn_exp2f(M[x] - m);
+                    M[x] = m;
+                    l[x] *= keep;
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) acc[x][j] *= keep * shift;
+                }
+            }
+            const float unit = __builtin_ldexpf(1.0f, 12 - E);
+            uint32_t w2[RT][NB][2];                         // weights, two to a word
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    float wv[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[x][n][r], rowc[x], -M[x]));
+                        wv[r] = pr * (__int_as_float(svw[n][r] & -16) * unit);
+                        if (!whole) {
+                            const bool in = live >> (x * 16 + 4 * n + r) & 1u;
+                            pr = in ? pr : 0.0f;
+                            wv[r] = in ? wv[r] : 0.0f;
+                        }
+                        l[x] += pr;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const v2h pair = __builtin_convertvector((v2f{wv[2 * i], wv[2 * i + 1]}), v2h);
+                        w2[x][n][i] = __builtin_bit_cast(uint32_t, pair);
+                    }
+                }
+            // ---- the product with the Values, 32 tokens at a time
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                v8h wop[RT];
+#pragma unroll
+                for (int x = 0; x < RT; ++x) {
+                    v4u o;
+                    if (NB == 4) {
+                        o = v4u{w2[x][2 * half][0], w2[x][2 * half][1], w2[x][2 * half + 1][0], w2[x][2 * half + 1][1]};
+                    } else if (NB == 2) {                   // block 2 half + 1 lies eight lanes on
+                        o = v4u{w2[x][half][0], w2[x][half][1], (uint32_t)dpp_i32<DPP_ROW_ROR8>((int)w2[x][half][0]),
+                                (uint32_t)dpp_i32<DPP_ROW_ROR8>((int)w2[x][half][1])};
+                    } else {                                // blocks 1, 2, 3 four, eight, twelve lanes on
+                        const int a = (int)w2[x][0][0], b2 = (int)w2[x][0][1];
+                        if (half == 0)
+                            o = v4u{(uint32_t)a, (uint32_t)b2, (uint32_t)dpp_i32<0x12C>(a), (uint32_t)dpp_i32<0x12C>(b2)};
+                        else
+                            o = v4u{(uint32_t)dpp_i32<DPP_ROW_ROR8>(a), (uint32_t)dpp_i32<DPP_ROW_ROR8>(b2),
+                                    (uint32_t)dpp_i32<DPP_ROW_ROR4>(a), (uint32_t)dpp_i32<DPP_ROW_ROR4>(b2)};
+                    }
+                    wop[x] = __builtin_bit_cast(v8h, o);
+                }
+#pragma unroll
+                for (int v = 0; v < VW; ++v) {
+                    uint32_t lo4[8], hi4[8], lut[8];
+                    v2h zero[4];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int k = 2 * half + i / 4, r = i % 4;
+                        const uint32_t hi = lut[i] = kv_lut_hi(vw[k][r]);
+                        if (Shape::HALVES) {
+                            lo4[i] = kv_bytes(vraw[k][r][v] >> (col >= 8 ? 4 : 0), hi);
+                        } else {
+                            lo4[i] = kv_bytes(vraw[k][r][v], hi);
+                            hi4[i] = kv_bytes(vraw[k][r][v] >> 4, hi);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)             // 16 z + 8 of two tokens
+                        zero[i] = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(lut[2 * i + 1], lut[2 * i], 0x0c070c03u) | 0x00080008u);
+#pragma unroll
+                    for (int j = 0; j < (Shape::HALVES ? 4 : 8); ++j) {
+                        const uint32_t sel = 0x0c040c00u + (uint32_t)(j & 3) * 0x00010001u;
+                        v4u n;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t two = j < 4 ? __builtin_amdgcn_perm(lo4[2 * i + 1], lo4[2 * i], sel) : __builtin_amdgcn_perm(hi4[2 * i + 1], hi4[2 * i], sel);
+                            n[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, two) - zero[i]);
+                        }
+#pragma unroll
+                        for (int x = 0; x < RT; ++x)
+                            acc[x][v * 8 + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, n), wop[x], acc[x][v * 8 + j], 0, 0, 0);
+                    }
+                }
+            }
+            if (more) {
+                load_v();
+                ask_pages();
+                ok = ok_next;
+            }
+        }
+    }
+
+    // ---- the waves' parts join: [NW][ROWS] maxima and sums, [NW][ROWS][D + 4] outputs
+    float *ml = lds, *os = lds + NW * ROWS * 2;
+    constexpr int LD = D + 4;
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+#pragma unroll
+        for (int d = RP; d < 64; d <<= 1) {
+            l[x] += __shfl_xor(l[x], d);
+        }
+        const int r = x * 16 + col;
+        if (col < RP) {
+            if (kg == 0) {
+                ml[(wave * ROWS + r) * 2] = M[x];
+                ml[(wave * ROWS + r) * 2 + 1] = l[x];
+            }
+            const int power = E + 8;                         // 2^24 for the operands, 1/16 for the unit, 2^(E - 12) for the weights
+            float *dst = os + (wave * ROWS + r) * LD;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int m = 4 * kg + i;
+                    const int ch = Shape::HALVES ? 8 * (m & 7) + 4 * (m >> 3) + j : 8 * VW * m + j;
+                    if (D != 96 || ch < 96) dst[ch] = __builtin_ldexpf(acc[x][j][i], power);
+                }
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < ROWS * D; i += NW * 64) {
+        const int r = i / D, ch = i - r * D, rr = row0 + r;
+        if (rr >= p.rows) continue;
+        float m = KV_NONE, sum = 0.0f, o = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, ml[(w * ROWS + r) * 2]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = __builtin_amdgcn_exp2f(ml[(w * ROWS + r) * 2] - m);
+            sum += f * ml[(w * ROWS + r) * 2 + 1];
+            o += f * os[(w * ROWS + r) * LD + ch];
+        }
+        const int s = rr / group;
+        if (p.splits == 1) {
+            const int64_t at = ((int64_t)b * t.S + s) * p.a.Hq + h * group + (rr - s * group);
+            ((T *)p.a.out)[at * D + ch] = attn_from_f32<T>(s < len.count && sum > 0.0f ? o / sum : 0.0f);
+        } else {
+            const int64_t at = (((int64_t)b * c.heads + h) * p.rows + rr) * p.splits + split;
+            if (s >= len.count) sum = 0.0f;
+            if (sum > 0.0f) p.part_o[at * D + ch] = o;
+            if (ch == 0) {
+                p.part_ml[at * 2] = m;
+                p.part_ml[at * 2 + 1] = sum;
+            }
+        }
+    }
+}
+
+// Joins the splits: a workgroup per (sequence, head, row)
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_kernel(StreamArgs p, int heads, int S, int D)
+{
+    __shared__ float red[5][256];
+    const int64_t at = blockIdx.x;
+    const int rr = (int)(at % p.rows);
+    const int64_t bh = at / p.rows;
+    const int h = (int)(bh % heads), tid = threadIdx.x;
+    const int64_t b = bh / heads;
+    const float *ml = p.part_ml + at * p.splits * 2, *po = p.part_o + at * p.splits * D;
+    float m = KV_NONE;
+    for (int s = tid & 63; s < p.splits; s += 64) m = ml[2 * s + 1] > 0.0f ? fmaxf(m, ml[2 * s]) : m;
+    m = wave_max(m);
+    const int s0 = rr / p.a.group;
+    const int64_t out = (b * S + s0) * p.a.Hq + h * p.a.group + (rr - s0 * p.a.group);
+    const int quad = D / 4, ways = 256 / quad, way = tid / quad, ch = (tid - way * quad) * 4;
+    float sum = 0.0f;
+    v4f o = {0, 0, 0, 0};
+    if (way < ways) {
+        for (int s = way; s < p.splits; s += ways) {
+            const float ls = ml[2 * s + 1];
+            if (ls > 0.0f) {
+                const float f = __builtin_amdgcn_exp2f(ml[2 * s] - m);
+                sum += f * ls;
+                o += *reinterpret_cast<const v4f *>(po + (int64_t)s * D + ch) * f;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[i][tid] = o[i];
+    red[4][tid] = sum;
+    __syncthreads();
+    if (tid < quad) {
+        for (int w = 1; w < ways; ++w) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] += red[i][tid + w * quad];
+            sum += red[4][tid + w * quad];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ((T *)p.a.out)[out * D + ch + i] = attn_from_f32<T>(sum > 0.0f ? o[i] / sum : 0.0f);
+    }
+}
+
 template <typename T>
 static int launch_attn_t(const AttnArgs &p, const KvView &c, const KvTokens &t, hipStream_t st)
 {
@@ -102,14 +613,108 @@ static int launch_attn_t(const AttnArgs &p, const KvView &c, const KvTokens &t, 
     return hip_status(hipGetLastError());
 }
 
-size_t attention_kv_workspace(int, const KvView &, const KvTokens &, int, int64_t) { return 0; }
+// ---- which kernel, and how the work is cut ---------------------------------------------------------------------------------------
+struct AttnPlan {
+    int stream;              // the streaming kernel's tiles of 16 rows (1 or 2); 0: a workgroup per row
+    int rp, waves;
+    int row_tiles, splits, chunk;
+    size_t part_bytes, ml_bytes;
+};
+constexpr size_t ATTN_ALIGN = 256;
+
+static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, int Hq, int64_t max_len)
+{
+    AttnPlan n = {};
+    n.splits = 1;
+    const int64_t rows = (int64_t)t.S * (Hq / c.heads);
+    const bool pages = c.page_size % 16 == 0 && c.page_ld % 16 == 0 && c.head_ld % 16 == 0 && c.pages > 0 && t.table_cols > 0;
+    if (dtype == W4A8_F32 || !pages || (c.D != 64 && c.D != 96 && c.D != 128 && c.D != 256) || rows > 32) return n;
+    n.stream = rows <= 16 || c.D == 256 ? 1 : 2;
+    n.rp = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+    n.waves = 8;
+    n.row_tiles = (int)((rows + 16 * n.stream - 1) / (16 * n.stream));
+    const int64_t tokens = std::max<int64_t>(1, std::min<int64_t>(max_len, (int64_t)t.table_cols * c.page_size));
+    const int64_t pairs = (int64_t)t.B * c.heads, tile = n.waves * 64;
+    const int64_t want = std::max<int64_t>(1, 1024 / pairs), most = (tokens + 2 * tile - 1) / (2 * tile);
+    const int64_t splits = std::min(want, most);
+    n.chunk = (int)(((tokens + splits - 1) / splits + 63) / 64 * 64);
+    n.splits = (int)((tokens + n.chunk - 1) / n.chunk);
+    if (n.splits > 1) {
+        const size_t parts = (size_t)pairs * rows * n.splits;
+        n.part_bytes = (parts * c.D * 4 + ATTN_ALIGN - 1) / ATTN_ALIGN * ATTN_ALIGN;
+        n.ml_bytes = parts * 8;
+    }
+    return n;
+}
+
+size_t attention_kv_workspace(int dtype, const KvView &c, const KvTokens &t, int Hq, int64_t max_len)
+{
+    const AttnPlan n = plan_attention(dtype, c, t, Hq, max_len);
+    return n.part_bytes + n.ml_bytes;
+}
+
+template <typename T, int D, int RP, int RT>
+static int launch_stream(const StreamArgs &p, const KvView &c, const KvTokens &t, hipStream_t st)
+{
+    constexpr int NW = 8, ROWS = RP * RT;
+    constexpr int bytes = NW * ROWS * (2 + D + 4) * 4;
+    static std::atomic<uint64_t> done{0};
+    if (bytes > 65536) {
+        const int rc = opt_in_dynamic_lds((const void *)attn_stream_kernel<T, D, RP, RT, NW>, bytes, done);
+        if (rc != W4A8_OK) return rc;
+    }
+    const int64_t blocks = (int64_t)t.B * c.heads * p.row_tiles * p.splits;
+    if (blocks > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+    hipLaunchKernelGGL((attn_stream_kernel<T, D, RP, RT, NW>), dim3((unsigned)blocks), dim3(NW * 64), bytes, st, p, c, t);
+    if (p.splits > 1)
+        hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)((int64_t)t.B * c.heads * p.rows)), dim3(256), 0, st, p, c.heads, t.S, c.D);
+    return hip_status(hipGetLastError());
+}
+
+template <typename T, int D>
+static int launch_stream_d(const AttnPlan &n, const StreamArgs &p, const KvView &c, const KvTokens &t, hipStream_t st)
+{
+    if (n.stream == 2) {
+        if constexpr (D <= 128) return launch_stream<T, D, 16, 2>(p, c, t, st);
+        return W4A8_ERR_SHAPE;
+    }
+    if (n.rp == 4) return launch_stream<T, D, 4, 1>(p, c, t, st);
+    if (n.rp == 8) return launch_stream<T, D, 8, 1>(p, c, t, st);
+    return launch_stream<T, D, 16, 1>(p, c, t, st);
+}
+
+template <typename T>
+static int launch_stream_t(const AttnPlan &n, const AttnArgs &a, const KvView &c, const KvTokens &t, void *workspace, hipStream_t st)
+{
+    StreamArgs p;
+    p.a = a;
+    p.part_o = (float *)workspace;
+    p.part_ml = (float *)((uint8_t *)workspace + n.part_bytes);
+    p.rows = t.S * a.group;
+    p.row_tiles = n.row_tiles;
+    p.splits = n.splits;
+    p.chunk = n.chunk;
+    p.page_jump = n.waves * 64 / c.page_size;
+    p.page_rest = n.waves * 64 % c.page_size;
+    p.q_vec = (uintptr_t)a.q % 16 == 0 && (a.q_ld_b | a.q_ld_s | a.q_ld_h) % 8 == 0;
+    switch (c.D) {
+        case 64: return launch_stream_d<T, 64>(n, p, c, t, st);
+        case 96: return launch_stream_d<T, 96>(n, p, c, t, st);
+        case 128: return launch_stream_d<T, 128>(n, p, c, t, st);
+        case 256: return launch_stream_d<T, 256>(n, p, c, t, st);
+        default: return W4A8_ERR_SHAPE;
+    }
+}
 
 int launch_attention_kv(const void *Q, const int64_t *q_ld, int dtype, int Hq, const KvView &c, const KvTokens &t, float scale,
-                        int64_t max_len, void *out, void *, hipStream_t st)
+                        int64_t max_len, void *out, void *workspace, hipStream_t st)
 {
     const int64_t room = (int64_t)t.table_cols * c.page_size;
     const AttnArgs p = {Q, out, q_ld[0], q_ld[1], q_ld[2], Hq, Hq / c.heads, (int)(max_len < room ? max_len : room),
                         scale * 1.44269504088896341f};
+    const AttnPlan n = plan_attention(dtype, c, t, Hq, max_len);
+    if (n.stream)
+        return dtype == W4A8_F16 ? launch_stream_t<__half>(n, p, c, t, workspace, st) : launch_stream_t<bf16_t>(n, p, c, t, workspace, st);
     switch (dtype) {
         case W4A8_F32: return launch_attn_t<float>(p, c, t, st);
         case W4A8_F16: return launch_attn_t<__half>(p, c, t, st);

@@ -10,9 +10,9 @@
 namespace w4a8 {
 
 struct KvView {
-    uint8_t *packed[2];     // Keys, Values: [pages][heads][page_size][D / 2]
+    uint8_t *packed[2];     // Keys, Values: [pages][heads][page_size][D / 2], the last two contiguous
     int32_t *words[2];      // [pages][heads][page_size]
-    int64_t pages;
+    int64_t pages, page_ld, head_ld;    // (ld: in rows)
     int heads, page_size, D;
 };
 struct KvTokens {
@@ -36,12 +36,12 @@ __device__ __forceinline__ KvLength kv_length(const KvTokens &t, const KvView &c
     return n;
 }
 
-// The index of a token's row ((page, head, place) flattened); -1 where the table names no page of the cache.
+// The index of a token's row; -1 where the table names no page of the cache.
 __device__ __forceinline__ int64_t kv_row(const KvTokens &t, const KvView &c, int b, int head, int token)
 {
     const int j = token / c.page_size;
     const int64_t page = t.table[b * t.table_ld + j];
-    return page < 0 || page >= c.pages ? -1 : (page * c.heads + head) * c.page_size + (token - j * c.page_size);
+    return page < 0 || page >= c.pages ? -1 : page * c.page_ld + head * c.head_ld + (token - j * c.page_size);
 }
 
 // One word's eight values in units of step / 8: the decode of the packed weights (D = 4 (d + beta), unsigned bytes), widened.

@@ -341,9 +341,18 @@ bool kv_operands(PyObject *const *c, PyObject *const *t, w4a8_kv_cache &cache, w
     for (int i = 0; i < 4; ++i) {
         const at::Tensor &x = THPVariable_Unpack(c[i]);
         const bool words = i & 1;
-        if (x.dim() != (words ? 3 : 4) || !x.is_contiguous() || x.scalar_type() != (words ? at::kInt : at::kByte) || x.device() != device) return false;
+        if (x.dim() != (words ? 3 : 4) || x.scalar_type() != (words ? at::kInt : at::kByte) || x.device() != device) return false;
         for (int d = 0; d < x.dim(); ++d)
             if (x.size(d) != kp.size(d)) return false;
+        // rows contiguous in a (page, head), and as far apart in all four (a dimension of one has no distance)
+        const int64_t row = words ? 1 : kp.size(3), page = x.size(0) > 1 ? x.stride(0) : 0, head = x.size(1) > 1 ? x.stride(1) : 0;
+        if (row < 1 || (!words && row > 1 && x.stride(3) != 1) || (x.size(2) > 1 && x.stride(2) != row) || page % row != 0 || head % row != 0) return false;
+        if (i == 0) {
+            cache.page_ld = page / row;
+            cache.head_ld = head / row;
+        } else if (cache.page_ld != page / row || cache.head_ld != head / row) {
+            return false;
+        }
     }
     cache.k_packed = (uint8_t *)kp.data_ptr();
     cache.k_words = (int32_t *)ptr(c[1]);

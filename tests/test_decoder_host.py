@@ -21,7 +21,7 @@ Z = ctypes.c_void_p(0)
 
 
 def cache_args(**kw):
-    d = dict(k_packed=0x1000, k_words=0x2000, v_packed=0x3000, v_words=0x4000, pages=8, heads=4, page_size=16, head_dim=128)
+    d = dict(k_packed=0x1000, k_words=0x2000, v_packed=0x3000, v_words=0x4000, pages=8, heads=4, page_size=16, head_dim=128, page_ld=64, head_ld=16)
     return b._KVCacheArgs(**{**d, **kw})
 
 
@@ -49,7 +49,7 @@ def test_norm_refusals(lib):
 
 @pytest.mark.parametrize("bad,status", [
     (dict(heads=0), b.ERR_SHAPE), (dict(page_size=0), b.ERR_SHAPE), (dict(head_dim=0), b.ERR_SHAPE), (dict(head_dim=60), b.ERR_SHAPE),
-    (dict(head_dim=520), b.ERR_SHAPE), (dict(pages=-1), b.ERR_SHAPE), (dict(page_size=1 << 30), b.ERR_SHAPE),
+    (dict(head_dim=520), b.ERR_SHAPE), (dict(page_ld=-1), b.ERR_SHAPE), (dict(head_ld=-1), b.ERR_SHAPE), (dict(pages=-1), b.ERR_SHAPE), (dict(page_size=1 << 30), b.ERR_SHAPE),
     (dict(k_packed=0), b.ERR_NULL), (dict(v_words=0), b.ERR_NULL), (dict(k_packed=0x1008), b.ERR_SHAPE), (dict(v_words=0x4004), b.ERR_SHAPE)])
 def test_cache_refusals(lib, bad, status):
     c, t = cache_args(**bad), token_args()
@@ -103,6 +103,8 @@ def test_python_checks():
     for kw in (dict(k=k[..., :32]), dict(k=k.float()), dict(v=k[:2]), dict(k=k[:, :, :1], v=k[:, :, :1]), dict(start=start.long()), dict(start=start[:2]),
                dict(count=count[:2]), dict(table=table.long()), dict(table=table[:2]), dict(table=table.t().contiguous().t()),
                dict(cache=cache._replace(k_words=cache.k_words[:2])), dict(cache=cache._replace(v_packed=cache.v_packed.int())),
+               dict(cache=cache._replace(v_words=cache.v_words.transpose(0, 1).contiguous().transpose(0, 1))),
+               dict(cache=cache._replace(k_packed=cache.k_packed.transpose(2, 3).contiguous().transpose(2, 3))),
                dict(k=k.transpose(2, 3).contiguous().transpose(2, 3))):
         with pytest.raises(ValueError):
             w.kv_cache_write_dint4(**{**good, **kw})

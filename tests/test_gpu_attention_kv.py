@@ -176,6 +176,8 @@ def test_strides_forms_streams_graphs(S, G, D, monkeypatch):
     ref = check(q, cache, start, None, table)
     dev = w.KVCacheDint4(*(t.cuda() for t in cache))
     st, tb = torch.tensor(start, dtype=torch.int32).cuda(), table.cuda()
+    heads_first = w.KVCacheDint4(*(t.transpose(0, 1).contiguous().transpose(0, 1) for t in dev))
+    assert torch.equal(w.attention_kv_dint4(q.cuda(), heads_first, st, None, tb), ref)
     for pad in (0, 8, 3):                                # cut out of a fused projection's output
         fused = torch.zeros((B, S, (G + 2) * H * D + pad), dtype=torch.float16, device="cuda")
         qv = fused[..., pad:pad + G * H * D].unflatten(-1, (G * H, D))

@@ -140,6 +140,10 @@ def test_strides_streams_and_forms(monkeypatch):
     w.kv_cache_write_dint4(k.transpose(1, 2).contiguous().transpose(1, 2).cuda(), v.cuda(), got, start, count, table)
     assert all(torch.equal(a, b) for a, b in zip(got, ref))
     values = w.kv_cache_read_dint4(ref, start, S, count, table)
+    got = w.KVCacheDint4(*(t.transpose(0, 1).contiguous().transpose(0, 1) for t in fresh(8, H, P, D)))     # heads first
+    w.kv_cache_write_dint4(k.cuda(), v.cuda(), got, start, count, table)
+    assert all(torch.equal(a, b) for a, b in zip(got, ref))
+    assert all(torch.equal(a, b) for a, b in zip(w.kv_cache_read_dint4(got, start, S, count, table), values))
     st = torch.cuda.Stream()
     st.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(st):
