@@ -4,6 +4,7 @@
 //
 // with the h / (Hq / Hkv)-th head of the cache.  A query that is not there (i >= count[b]) gives zeros.
 #include <algorithm>
+#include <utility>
 
 #include "kv_dint4.hpp"
 
@@ -550,6 +551,370 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
     }
 }
 
+// ---- many query rows per head of the cache: tiles of decoded rows in LDS ----------------------------------------------------------
+//
+// A workgroup of NW waves has 32 NW rows (row r = token r / group, head r % group of the group), goes through the tokens 64 at
+// a time and decodes each tile of Keys and Values once for all of them: half of the waves the Keys, to [token][channel], half
+// the Values, to [channel][token], both as signed fp16 numbers (n - 16 z - 8) 2^-24 (see above: exact).  Each wave multiplies
+// its 32 rows on 32 x 32 tiles: scores as (tokens) x (rows), so that a lane has 32 of the tile's scores of one row; they are the
+// right operand of the product with the Values as they stand, the Values' tokens being put in that order.  A row's statistics
+// are its lane's (and the lane's 32 on), so rescaling needs no exchange either.  Steps differ from token to token, i.e. from
+// register to register: lane i of each 16 holds that of register i, and the multiplication takes it as a row broadcast.
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+template <int I> __device__ __forceinline__ float row_bcast(float v)     // lane I of the 16
+{
+    return dpp_f32<0x150 + I>(v);
+}
+template <int... I, typename F> __device__ __forceinline__ void unroll16(std::integer_sequence<int, I...>, F f)
+{
+    (f(std::integral_constant<int, I>()), ...);
+}
+
+// a word's eight halves, (n - 16 z - 8) 2^-24
+__device__ __forceinline__ v4u kv_halves(uint32_t p, int32_t word)
+{
+    const uint32_t hi = kv_lut_hi(word), lo4 = kv_bytes(p, hi), hi4 = kv_bytes(p >> 4, hi);
+    const v2h zero = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0u, hi, 0x0c030c03u) | 0x00080008u);
+    const uint32_t n[4] = {__builtin_amdgcn_perm(0u, lo4, 0x0c010c00u), __builtin_amdgcn_perm(0u, lo4, 0x0c030c02u),
+                           __builtin_amdgcn_perm(0u, hi4, 0x0c010c00u), __builtin_amdgcn_perm(0u, hi4, 0x0c030c02u)};
+    v4u o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, n[i]) - zero);
+    return o;
+}
+
+// 16-byte chunk of a channel's row of 64 tokens in LDS: spread so that neither 16 channels in a row (the product's reads) nor
+// 16 channels eight apart (the decoder's writes) meet in a bank more often than they must
+__device__ __forceinline__ int v_chunk(int ch, int chunk) { return chunk ^ (((ch >> 1) ^ (ch >> 3)) & 7); }
+
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p, KvView c, KvTokens t)
+{
+    constexpr int KLD = D * 2 + 16, KBYTES = 64 * KLD, VBYTES = D * 128, BUF = KBYTES + VBYTES;
+    constexpr int KS = D / 16, CB = D / 32, WORDS = D / 8;
+    constexpr int HALF = NW / 2 * 64;                       // threads that decode Keys; as many decode Values
+    constexpr int KT = (64 * WORDS + HALF - 1) / HALF;      // words per thread (Keys)
+    constexpr int VT = (16 * WORDS + HALF - 1) / HALF;      // words of four tokens per thread (Values)
+    extern __shared__ uint8_t tile_lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, kg = lane >> 5;
+    int id = blockIdx.x;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int bh = id % (t.B * c.heads), rt = p.row_tiles - 1 - id / (t.B * c.heads);   // (longest first)
+    const int h = bh % c.heads, b = bh / c.heads;
+    const int group = p.a.group, row0 = rt * NW * 32, wrow0 = row0 + wave * 32;
+    const KvLength len = kv_length(t, c, b);
+    auto limit = [&](int r) { return min(len.start + r / group + 1, p.a.max_len); };    // tokens that a row sees, if it is there
+    const int there = min(p.rows, len.count * group);                                   // rows that are there
+    const int lim_wg = row0 < there ? limit(min(row0 + NW * 32, there) - 1) : 0;
+    const int lim_hi = wrow0 < there ? limit(min(wrow0 + 32, there) - 1) : 0, lim_lo = wrow0 < there ? limit(wrow0) : 0;
+    const int t0 = split * p.chunk, t1 = min(lim_wg, t0 + p.chunk);
+    const int my_row = wrow0 + col;
+    const int lim = my_row < there ? limit(my_row) : lim_hi;
+
+    float M = KV_NONE, l = 0.0f;
+    int E = -114;
+    v16f acc[CB];
+#pragma unroll
+    for (int k = 0; k < CB; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[k][i] = 0.0f;
+
+    if (t0 < t1) {
+        // ---- queries
+        v8h q[KS];
+        float rowc;
+        {
+            const int r = min(my_row, p.rows - 1), s = r / group;
+            const T *src = (const T *)p.a.q + b * p.a.q_ld_b + s * p.a.q_ld_s + (h * group + (r - s * group)) * p.a.q_ld_h + kg * 8;
+            float top = 0.0f;
+            uint32_t raw[KS][4];
+#pragma unroll
+            for (int j = 0; j < KS; ++j) {
+                float f[8];
+                load_q8<T>(src + 16 * j, p.q_vec, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw[j][i] = (uint32_t)__builtin_bit_cast(uint16_t, attn_from_f32<T>(f[2 * i])) |
+                                                        (uint32_t)__builtin_bit_cast(uint16_t, attn_from_f32<T>(f[2 * i + 1])) << 16;
+            }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float power = q_power<T>(top), turn = p.a.scale_log2 < 0.0f ? -power : power;
+#pragma unroll
+            for (int j = 0; j < KS; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    q[j][i] = (_Float16)(to_f32(__builtin_bit_cast(T, (uint16_t)(raw[j][i / 2] >> (i & 1) * 16))) * turn);
+            rowc = fabsf(p.a.scale_log2) * 0x1p20f / power;
+        }
+
+        // ---- the tiles' rows
+        const int32_t *table = t.table + b * t.table_ld;
+        int page_j[4], page_off[4];
+        int32_t page[4];
+        int64_t row[4];
+        uint32_t ok = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            page_j[k] = (t0 + 16 * k) / c.page_size;
+            page_off[k] = t0 + 16 * k - page_j[k] * c.page_size;
+        }
+        auto ask_pages = [&]() {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) page[k] = table[min(page_j[k], t.table_cols - 1)];
+        };
+        auto place_rows = [&]() {                           // (blocks past the table are past every row's limit too)
+            ok = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool good = page[k] >= 0 && page[k] < c.pages;
+                ok |= good ? 1u << k : 0u;
+                row[k] = (good ? page[k] * c.page_ld + page_off[k] : 0) + h * c.head_ld;
+                page_j[k] += p.page_jump;
+                page_off[k] += p.page_rest;
+                if (page_off[k] >= c.page_size) {
+                    page_off[k] -= c.page_size;
+                    ++page_j[k];
+                }
+            }
+        };
+        auto block_row = [&](int blk) {                     // row of a lane's own block of 16 tokens
+            int64_t at = row[0];
+#pragma unroll
+            for (int k = 1; k < 4; ++k) at = blk == k ? row[k] : at;
+            return at;
+        };
+        // what this thread decodes of the next tile, as it comes from memory
+        const bool keys = wave < NW / 2;
+        const int part = keys ? tid : tid - HALF;
+        uint32_t raw[KT > 4 * VT ? KT : 4 * VT];
+        int32_t rw[KT > 4 * VT ? KT : 4 * VT];
+        int32_t stw[2][2];                                  // words of Keys and Values for the softmax: lane i & 15's token of block 0, 1
+        int tile_ok[2];                                     // which of them count
+        auto load_tile = [&](int tok) {
+            if (keys) {
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    const int w = min(part + k * HALF, 64 * WORDS - 1), tk = w / WORDS;
+                    const int64_t at = block_row(tk >> 4) + (tk & 15);
+                    raw[k] = reinterpret_cast<const uint32_t *>(c.packed[0])[at * WORDS + (w - tk * WORDS)];
+                    rw[k] = c.words[0][at];
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < VT; ++k) {
+                    const int w = min(part + k * HALF, 16 * WORDS - 1), tq = w / WORDS;
+                    const int64_t at = block_row(tq >> 2) + 4 * (tq & 3);
+                    const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[1]) + at * WORDS + (w - tq * WORDS);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) raw[4 * k + r] = src[r * WORDS];
+                    const v4i z = *reinterpret_cast<const v4i *>(c.words[1] + at);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) rw[4 * k + r] = z[r];
+                }
+            }
+            const int i = lane & 15;
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                const int tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
+                const int64_t at = (i & 8 ? row[2 * tb + 1] : row[2 * tb]) + (tk & 15);
+                stw[tb][0] = c.words[0][at];
+                stw[tb][1] = c.words[1][at];
+                tile_ok[tb] = tok + tk < t1 && (ok >> (2 * tb + (i >> 3)) & 1u);
+            }
+        };
+        auto decode_tile = [&](uint8_t *buf) {
+            if (keys) {
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    const int w = part + k * HALF, tk = w / WORDS;
+                    if (64 * WORDS % HALF == 0 || w < 64 * WORDS)
+                        *reinterpret_cast<v4u *>(buf + tk * KLD + (w - tk * WORDS) * 16) = kv_halves(raw[k], rw[k]);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < VT; ++k) {
+                    const int w = part + k * HALF, tq = w / WORDS, m = w - tq * WORDS;
+                    if (16 * WORDS % HALF == 0 || w < 16 * WORDS) {
+                        uint32_t lo4[4], hi4[4], lut[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            lut[r] = kv_lut_hi(rw[4 * k + r]);
+                            lo4[r] = kv_bytes(raw[4 * k + r], lut[r]);
+                            hi4[r] = kv_bytes(raw[4 * k + r] >> 4, lut[r]);
+                        }
+                        v2h zero[2];
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            zero[r] = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(lut[2 * r + 1], lut[2 * r], 0x0c070c03u) | 0x00080008u);
+                        const int chunk = 2 * (tq >> 2) + (tq & 1), off = 8 * ((tq >> 1) & 1);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint32_t sel = 0x0c040c00u + (uint32_t)(j & 3) * 0x00010001u;
+                            v2u o;
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const uint32_t two = j < 4 ? __builtin_amdgcn_perm(lo4[2 * r + 1], lo4[2 * r], sel) : __builtin_amdgcn_perm(hi4[2 * r + 1], hi4[2 * r], sel);
+                                o[r] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, two) - zero[r]);
+                            }
+                            const int ch = 8 * m + j;
+                            *reinterpret_cast<v2u *>(buf + KBYTES + ch * 128 + v_chunk(ch, chunk) * 16 + off) = o;
+                        }
+                    }
+                }
+            }
+        };
+
+        ask_pages();
+        place_rows();
+        load_tile(t0);
+        ask_pages();
+        int buf = 0;
+        for (int tok = t0; tok < t1; tok += 64) {
+            uint8_t *lds = tile_lds + buf * BUF;
+            buf ^= 1;
+            decode_tile(lds);
+            const uint32_t ok_now = ok;
+            float sk[2], sv[2];
+            uint32_t top_step = 0;
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                sk[tb] = tile_ok[tb] ? kv_step(stw[tb][0]) : 0.0f;
+                sv[tb] = tile_ok[tb] ? fabsf(kv_step(stw[tb][1])) : 0.0f;
+                top_step = max(top_step, __float_as_uint(sv[tb]));
+            }
+            if (tok + 64 < t1) {
+                place_rows();
+                load_tile(tok + 64);
+                ask_pages();
+            }
+            __syncthreads();        // (one barrier a tile: the other buffer's readers are behind the last one)
+            if (tok >= lim_hi) continue;
+            const bool whole = ok_now == 15u && tok + 64 <= lim_lo;
+
+            v16f y[2];
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[tb][i] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < KS; ++j) {
+                    const v8h a = *reinterpret_cast<const v8h *>(lds + (tb * 32 + col) * KLD + j * 32 + kg * 16);
+                    y[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[j], y[tb], 0, 0, 0);
+                }
+            }
+            float top = KV_MASKED;
+            uint32_t live = ~0u;
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+                unroll16(std::make_integer_sequence<int, 16>(), [&](auto ic) {
+                    constexpr int i = decltype(ic)::value;
+                    y[tb][i] *= row_bcast<i>(sk[tb]);
+                });
+            if (!whole) {
+                live = 0;
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
+                        const bool in = tok + tk < lim && (ok_now >> (2 * tb + (i >> 3)) & 1u);
+                        live |= in ? 1u << (tb * 16 + i) : 0u;
+                        y[tb][i] = in ? y[tb][i] : KV_MASKED;
+                    }
+            }
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, y[tb][i]);
+            top *= rowc;
+            const bool move = (int)(top_step >> 23) - 127 > E || top > M + KV_SLACK;
+            if (__builtin_amdgcn_ballot_w64(move)) {        // rare: another maximum, or a larger step
+                uint32_t e = top_step >> 23;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) e = max(e, (uint32_t)__shfl_xor((int)e, d));
+                const int E_new = max(E, (int)e - 127);
+                float m = fmaxf(top, M);
+                m = fmaxf(m, __shfl_xor(m, 32));
+                const float keep = __builtin_amdgcn_exp2f(M - m), both = __builtin_ldexpf(keep, E - E_new);
+                E = __builtin_amdgcn_readfirstlane(E_new);
+                M = m;
+                l *= keep;
+#pragma unroll
+                for (int k = 0; k < CB; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[k][i] *= both;
+            }
+            const float unit = __builtin_ldexpf(1.0f, 12 - E);
+            v4u w[4];
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                const float svn = sv[tb] * unit;
+                float wv[16];
+                unroll16(std::make_integer_sequence<int, 16>(), [&](auto ic) {
+                    constexpr int i = decltype(ic)::value;
+                    float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[tb][i], rowc, -M));
+                    if (!whole) pr = live >> (tb * 16 + i) & 1u ? pr : 0.0f;
+                    l += pr;
+                    wv[i] = pr * row_bcast<i>(svn);
+                });
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[2 * tb + i / 4][i & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{wv[2 * i], wv[2 * i + 1]}), v2h));
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int k = 0; k < CB; ++k) {
+                    const int ch = k * 32 + col;
+                    const v8h a = *reinterpret_cast<const v8h *>(lds + KBYTES + ch * 128 + v_chunk(ch, 2 * s + kg) * 16);
+                    acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(v8h, w[s]), acc[k], 0, 0, 0);
+                }
+        }
+    }
+
+    if (my_row >= p.rows) return;
+    l += __shfl_xor(l, 32);                                 // (lanes 32 apart have the same row)
+    const int s = my_row / group, power = E + 8;            // 2^24 for the operands, 1/16 for the unit, 2^(E - 12) for the weights
+    if (s >= len.count) l = 0.0f;
+    if (p.splits == 1) {
+        T *out = (T *)p.a.out + (((int64_t)b * t.S + s) * p.a.Hq + h * group + (my_row - s * group)) * D;
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+        for (int k = 0; k < CB; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint16_t o[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float v = l > 0.0f ? __builtin_ldexpf(acc[k][4 * i + r], power) * inv : 0.0f;
+                    o[r] = __builtin_bit_cast(uint16_t, attn_from_f32<T>(v));
+                }
+                *reinterpret_cast<v2u *>(out + k * 32 + 8 * i + 4 * kg) = v2u{(uint32_t)o[0] | (uint32_t)o[1] << 16, (uint32_t)o[2] | (uint32_t)o[3] << 16};
+            }
+    } else {
+        const int64_t at = (((int64_t)b * c.heads + h) * p.rows + my_row) * p.splits + split;
+        if (l > 0.0f) {
+#pragma unroll
+            for (int k = 0; k < CB; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v4f o;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[r] = __builtin_ldexpf(acc[k][4 * i + r], power);
+                    *reinterpret_cast<v4f *>(p.part_o + at * D + k * 32 + 8 * i + 4 * kg) = o;
+                }
+        }
+        if (kg == 0) {
+            p.part_ml[at * 2] = M;
+            p.part_ml[at * 2 + 1] = l;
+        }
+    }
+}
+
 // Joins the splits: a workgroup per (sequence, head, row)
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_kernel(StreamArgs p, int heads, int S, int D)
@@ -615,7 +980,8 @@ static int launch_attn_t(const AttnArgs &p, const KvView &c, const KvTokens &t, 
 
 // ---- which kernel, and how the work is cut ---------------------------------------------------------------------------------------
 struct AttnPlan {
-    int stream;              // the streaming kernel's tiles of 16 rows (1 or 2); 0: a workgroup per row
+    int stream;              // the streaming kernel's tiles of 16 rows (1 or 2); 0: another kernel
+    int tile;                // the tile kernel's waves; 0 and no stream: a workgroup per row
     int rp, waves;
     int row_tiles, splits, chunk;
     size_t part_bytes, ml_bytes;
@@ -628,22 +994,32 @@ static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, in
     n.splits = 1;
     const int64_t rows = (int64_t)t.S * (Hq / c.heads);
     const bool pages = c.page_size % 16 == 0 && c.page_ld % 16 == 0 && c.head_ld % 16 == 0 && c.pages > 0 && t.table_cols > 0;
-    if (dtype == W4A8_F32 || !pages || (c.D != 64 && c.D != 96 && c.D != 128 && c.D != 256) || rows > 32) return n;
+    if (dtype == W4A8_F32 || !pages || (c.D != 64 && c.D != 96 && c.D != 128 && c.D != 256)) return n;
+    if (rows > 0x7fffffffLL / 2) return n;
+    const int64_t tokens = std::max<int64_t>(1, std::min<int64_t>(max_len, (int64_t)t.table_cols * c.page_size));
+    const int64_t pairs = (int64_t)t.B * c.heads;
+    auto cut = [&](int64_t want, int64_t most) {
+        const int64_t splits = std::max<int64_t>(1, std::min(want, most));
+        n.chunk = (int)(((tokens + splits - 1) / splits + 63) / 64 * 64);
+        n.splits = (int)((tokens + n.chunk - 1) / n.chunk);
+        if (n.splits > 1) {
+            const size_t parts = (size_t)pairs * rows * n.splits;
+            n.part_bytes = (parts * c.D * 4 + ATTN_ALIGN - 1) / ATTN_ALIGN * ATTN_ALIGN;
+            n.ml_bytes = parts * 8;
+        }
+    };
+    if (rows > 32) {
+        n.tile = rows > 128 && c.D < 256 ? 8 : 4;
+        n.row_tiles = (int)((rows + 32 * n.tile - 1) / (32 * n.tile));
+        cut(256 / (pairs * n.row_tiles), tokens / 512);
+        return n;
+    }
     n.stream = rows <= 16 || c.D == 256 ? 1 : 2;
     n.rp = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
     n.waves = 8;
     n.row_tiles = (int)((rows + 16 * n.stream - 1) / (16 * n.stream));
-    const int64_t tokens = std::max<int64_t>(1, std::min<int64_t>(max_len, (int64_t)t.table_cols * c.page_size));
-    const int64_t pairs = (int64_t)t.B * c.heads, tile = n.waves * 64;
-    const int64_t want = std::max<int64_t>(1, 1024 / pairs), most = (tokens + 2 * tile - 1) / (2 * tile);
-    const int64_t splits = std::min(want, most);
-    n.chunk = (int)(((tokens + splits - 1) / splits + 63) / 64 * 64);
-    n.splits = (int)((tokens + n.chunk - 1) / n.chunk);
-    if (n.splits > 1) {
-        const size_t parts = (size_t)pairs * rows * n.splits;
-        n.part_bytes = (parts * c.D * 4 + ATTN_ALIGN - 1) / ATTN_ALIGN * ATTN_ALIGN;
-        n.ml_bytes = parts * 8;
-    }
+    const int64_t tile = n.waves * 64;
+    cut(1024 / pairs, (tokens + 2 * tile - 1) / (2 * tile));
     return n;
 }
 
@@ -671,9 +1047,30 @@ static int launch_stream(const StreamArgs &p, const KvView &c, const KvTokens &t
     return hip_status(hipGetLastError());
 }
 
+template <typename T, int D, int NW>
+static int launch_tile(const StreamArgs &p, const KvView &c, const KvTokens &t, hipStream_t st)
+{
+    constexpr int bytes = 2 * (64 * (D * 2 + 16) + D * 128);
+    static std::atomic<uint64_t> done{0};
+    if (bytes > 65536) {
+        const int rc = opt_in_dynamic_lds((const void *)attn_tile_kernel<T, D, NW>, bytes, done);
+        if (rc != W4A8_OK) return rc;
+    }
+    const int64_t blocks = (int64_t)t.B * c.heads * p.row_tiles * p.splits, joins = (int64_t)t.B * c.heads * p.rows;
+    if (blocks > 0x7fffffffLL || joins > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+    hipLaunchKernelGGL((attn_tile_kernel<T, D, NW>), dim3((unsigned)blocks), dim3(NW * 64), bytes, st, p, c, t);
+    if (p.splits > 1) hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)joins), dim3(256), 0, st, p, c.heads, t.S, c.D);
+    return hip_status(hipGetLastError());
+}
+
 template <typename T, int D>
 static int launch_stream_d(const AttnPlan &n, const StreamArgs &p, const KvView &c, const KvTokens &t, hipStream_t st)
 {
+    if (n.tile == 8) {
+        if constexpr (D <= 128) return launch_tile<T, D, 8>(p, c, t, st);
+        return W4A8_ERR_SHAPE;
+    }
+    if (n.tile == 4) return launch_tile<T, D, 4>(p, c, t, st);
     if (n.stream == 2) {
         if constexpr (D <= 128) return launch_stream<T, D, 16, 2>(p, c, t, st);
         return W4A8_ERR_SHAPE;
@@ -694,8 +1091,9 @@ static int launch_stream_t(const AttnPlan &n, const AttnArgs &a, const KvView &c
     p.row_tiles = n.row_tiles;
     p.splits = n.splits;
     p.chunk = n.chunk;
-    p.page_jump = n.waves * 64 / c.page_size;
-    p.page_rest = n.waves * 64 % c.page_size;
+    const int next = n.tile ? 64 : n.waves * 64;          // a wave's next tile, in tokens
+    p.page_jump = next / c.page_size;
+    p.page_rest = next % c.page_size;
     p.q_vec = (uintptr_t)a.q % 16 == 0 && (a.q_ld_b | a.q_ld_s | a.q_ld_h) % 8 == 0;
     switch (c.D) {
         case 64: return launch_stream_d<T, 64>(n, p, c, t, st);
@@ -713,7 +1111,7 @@ int launch_attention_kv(const void *Q, const int64_t *q_ld, int dtype, int Hq, c
     const AttnArgs p = {Q, out, q_ld[0], q_ld[1], q_ld[2], Hq, Hq / c.heads, (int)(max_len < room ? max_len : room),
                         scale * 1.44269504088896341f};
     const AttnPlan n = plan_attention(dtype, c, t, Hq, max_len);
-    if (n.stream)
+    if (n.stream || n.tile)
         return dtype == W4A8_F16 ? launch_stream_t<__half>(n, p, c, t, workspace, st) : launch_stream_t<bf16_t>(n, p, c, t, workspace, st);
     switch (dtype) {
         case W4A8_F32: return launch_attn_t<float>(p, c, t, st);
