@@ -96,9 +96,175 @@ __global__ __launch_bounds__(256) void norm_quant_generic_kernel(NormArgs p)
         p.q[m * (int64_t)p.K + k] = (int8_t)quant1_bits(to_f32(again[k]) * norm_gain<T>(p, k), inv);
 }
 
+// Eight values, rounded to the row's type (as they are kept) and packed; and their exact widening
+template <typename T> __device__ __forceinline__ Raw8<T> round8(const float (&v)[8])
+{
+    Raw8<T> o;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint16_t a = __builtin_bit_cast(uint16_t, from_f32<T>(v[2 * i])), b = __builtin_bit_cast(uint16_t, from_f32<T>(v[2 * i + 1]));
+        w[i] = (uint32_t)a | (uint32_t)b << 16;
+    }
+    o.v = make_uint4(w[0], w[1], w[2], w[3]);
+    return o;
+}
+template <> __device__ __forceinline__ Raw8<float> round8<float>(const float (&v)[8])
+{
+    Raw8<float> o;
+    o.a = make_float4(v[0], v[1], v[2], v[3]);
+    o.b = make_float4(v[4], v[5], v[6], v[7]);
+    return o;
+}
+template <typename T> __device__ __forceinline__ void store_raw8(T *p, const Raw8<T> &r) { *reinterpret_cast<uint4 *>(p) = r.v; }
+template <> __device__ __forceinline__ void store_raw8<float>(float *p, const Raw8<float> &r)
+{
+    reinterpret_cast<float4 *>(p)[0] = r.a;
+    reinterpret_cast<float4 *>(p)[1] = r.b;
+}
+
+// Rows of K % 8 == 0 elements on 16-byte aligned addresses: WPR waves to a row (one wave: four rows to a workgroup, no
+// barrier), NCH chunks of eight elements per lane.  The gains w / s are made once per workgroup and stay in registers, the row
+// stays in registers between the reduction and the rounding, and the next row's loads go out before this row is worked on:
+// one read of x and r, one write of h and Xq.
+template <typename T, int NCH, int WPR, bool RES>
+__global__ __launch_bounds__(WPR == 1 ? 256 : WPR * 64) void norm_quant_rows_kernel(NormArgs p)
+{
+    constexpr int LANES = WPR * 64, ROWS = WPR == 1 ? 4 : 1;
+    __shared__ float red[2][WPR];
+    __shared__ double red2[2][WPR];
+    const int tid = WPR == 1 ? threadIdx.x & 63 : threadIdx.x, sub = WPR == 1 ? threadIdx.x >> 6 : 0, wave = threadIdx.x >> 6;
+    const int chunks = p.K / 8;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    int64_t m = (int64_t)blockIdx.x * ROWS + sub;
+
+    Raw8<T> x[NCH], r[NCH];
+    auto load_row = [&](int64_t row) {
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int ch = tid + c * LANES;
+            if (ch < chunks) {
+                x[c] = load_raw8<T>((const T *)p.x + row * p.ldx + ch * 8);
+                if (RES) r[c] = load_raw8<T>((const T *)p.r + row * p.ldr + ch * 8);
+            }
+        }
+    };
+    if (m < p.M) load_row(m);
+    float gain[NCH][8];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) {
+        const int ch = tid + c * LANES;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) gain[c][j] = 0.0f;
+        if (ch < chunks) {
+            if (p.w_f32)
+                load8<float>((const float *)p.w + ch * 8, gain[c]);
+            else
+                load8<T>((const T *)p.w + ch * 8, gain[c]);
+            if (p.s) {
+                float s[8];
+                load8<float>(p.s + ch * 8, s);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) gain[c][j] *= 1.0f / s[j];
+            }
+        }
+    }
+    for (int flip = 0; m < p.M; m += step, flip ^= 1) {      // (uniform over a row's waves)
+        float t[NCH][8], a = 0.0f;
+        double ss = 0.0;
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int ch = tid + c * LANES;
+            float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (ch < chunks) {
+                widen8(x[c], f);
+                if (RES) {
+                    float g[8];
+                    widen8(r[c], g);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] += g[j];
+                    const Raw8<T> h = round8<T>(f);
+                    store_raw8<T>((T *)p.h + m * p.ldh + ch * 8, h);
+                    widen8(h, f);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                ss = __builtin_fma((double)f[j], (double)f[j], ss);
+                t[c][j] = f[j] * gain[c][j];
+                a = fmaxf(a, fabsf(t[c][j]));
+            }
+        }
+        if (m + step < p.M) load_row(m + step);
+        a = wave_max(a);
+        ss = wave_sum_f64(ss);
+        if (WPR > 1) {                                       // (two sets in turn: one barrier a row)
+            if ((tid & 63) == 0) {
+                red[flip][wave] = a;
+                red2[flip][wave] = ss;
+            }
+            __syncthreads();
+            a = red[flip][0];
+#pragma unroll
+            for (int w = 1; w < WPR; ++w) a = fmaxf(a, red[flip][w]);
+        }
+        const float inv = row_inverse(a);
+        if (tid == 0) {
+            if (WPR > 1) {
+                ss = red2[flip][0];
+#pragma unroll
+                for (int w = 1; w < WPR; ++w) ss += red2[flip][w];
+            }
+            p.sx[m] = row_scale(a, inv, ss, p);
+        }
+#pragma unroll
+        for (int c = 0; c < NCH; ++c) {
+            const int ch = tid + c * LANES;
+            if (ch < chunks) {
+                uint32_t b[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) b[j] = quant1_bits(t[c][j], inv);
+                *reinterpret_cast<uint2 *>(p.q + m * (int64_t)p.K + ch * 8) =
+                    make_uint2(pack4_low_bytes(b[0], b[1], b[2], b[3]), pack4_low_bytes(b[4], b[5], b[6], b[7]));
+            }
+        }
+    }
+}
+
+template <typename T, int NCH, int WPR>
+static int launch_rows(const NormArgs &p, int blocks_per_cu, hipStream_t st)
+{
+    constexpr int ROWS = WPR == 1 ? 4 : 1, THREADS = WPR == 1 ? 256 : WPR * 64;
+    const int64_t want = (p.M + ROWS - 1) / ROWS;
+    const dim3 grid((unsigned)(want < 256 * blocks_per_cu ? want : 256 * blocks_per_cu)), block(THREADS);
+    if (p.r)
+        hipLaunchKernelGGL((norm_quant_rows_kernel<T, NCH, WPR, true>), grid, block, 0, st, p);
+    else
+        hipLaunchKernelGGL((norm_quant_rows_kernel<T, NCH, WPR, false>), grid, block, 0, st, p);
+    return hip_status(hipGetLastError());
+}
+
 template <typename T>
 static int launch_norm_quant_t(const NormArgs &p, hipStream_t st)
 {
+    const auto off = [](const void *q, int64_t ld, int64_t elem) { return q && ((uintptr_t)q % 16 != 0 || ld * elem % 16 != 0); };
+    const bool vec = p.K % 8 == 0 && p.K <= 16384 && !off(p.x, p.ldx, sizeof(T)) && !off(p.r, p.ldr, sizeof(T)) && !off(p.h, p.ldh, sizeof(T)) &&
+                     (uintptr_t)p.w % 16 == 0 && (uintptr_t)p.s % 16 == 0 && (uintptr_t)p.q % 8 == 0;
+    if (vec) {
+        if (p.K <= 512) return launch_rows<T, 1, 1>(p, 8, st);
+        if (p.K <= 1024) return launch_rows<T, 2, 1>(p, 4, st);
+        if (p.M <= 512) {      // few rows: as many lanes to a row as there are chunks
+            if (p.K <= 2048) return launch_rows<T, 1, 4>(p, 8, st);
+            if (p.K <= 4096) return launch_rows<T, 1, 8>(p, 4, st);
+            if (p.K <= 8192) return launch_rows<T, 1, 16>(p, 2, st);
+            return launch_rows<T, 2, 16>(p, 2, st);
+        }
+        if (p.K <= 2048) return launch_rows<T, 1, 4>(p, 8, st);
+        if (p.K <= 4096) return launch_rows<T, 2, 4>(p, 4, st);
+        if (p.K <= 8192) return launch_rows<T, 2, 8>(p, 2, st);
+        if (p.K <= 12288) return launch_rows<T, 3, 8>(p, 2, st);
+        return launch_rows<T, 4, 8>(p, 1, st);
+    }
     hipLaunchKernelGGL((norm_quant_generic_kernel<T>), dim3((unsigned)p.M), dim3(256), 0, st, p);
     return hip_status(hipGetLastError());
 }
