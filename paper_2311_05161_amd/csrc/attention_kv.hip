@@ -151,6 +151,70 @@ template <> __device__ __forceinline__ float q_power<bf16_t>(float top)
     return __uint_as_float((uint32_t)min(268 - e, 253) << 23);
 }
 
+// ---- the rows of a tile of 64 tokens, four blocks of 16, block by block (page_size % 16 == 0, so a block lies in one page)
+//
+// All of it is uniform over the wave and stays in scalar registers: the table is read through the constant address space (no
+// kernel writes it), rows are numbered in 32 bits (the launcher checks that the cache has no more).
+typedef const __attribute__((address_space(4))) int32_t *scalar_i32;
+__device__ __forceinline__ scalar_i32 scalar_table(const int32_t *p) { return (scalar_i32)(uintptr_t)p; }
+
+// one of four values by a lane's own index (by value: a choice among array elements would send the array to memory)
+__device__ __forceinline__ uint32_t pick4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, int k)
+{
+    const uint32_t lo = k & 1 ? b : a, hi = k & 1 ? d : c;
+    return k & 2 ? hi : lo;
+}
+__device__ __forceinline__ uint32_t pick2(uint32_t a, uint32_t b, int k) { return k & 1 ? b : a; }
+
+struct TileRows {
+    scalar_i32 table;
+    int last, page_size, jump, rest;   // the table's last entry; a tile further is `jump` pages and `rest` tokens
+    uint32_t pages, page_ld, head;
+    int j[4], off[4];
+    int32_t page[4];
+    uint32_t row[4];                   // of each block's first token; the cache's own first page where there is none
+    uint32_t ok;                       // bit k: block k has a page
+
+    __device__ __forceinline__ TileRows(const KvView &c, const KvTokens &t, int b, int h, int token, int jump_, int rest_)
+    {
+        table = scalar_table(t.table + b * t.table_ld);
+        last = t.table_cols - 1;
+        page_size = c.page_size;
+        jump = jump_;
+        rest = rest_;
+        pages = (uint32_t)c.pages;
+        page_ld = (uint32_t)c.page_ld;
+        head = (uint32_t)h * (uint32_t)c.head_ld;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            j[k] = (int)((uint32_t)(token + 16 * k) / (uint32_t)page_size);
+            off[k] = token + 16 * k - j[k] * page_size;
+        }
+        ask();
+    }
+    // (blocks past the table are past every row's limit too: any page will do)
+    __device__ __forceinline__ void ask()
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) page[k] = table[min(j[k], last)];
+    }
+    // the rows of the tile asked for; then asks for the next one's pages
+    __device__ __forceinline__ void next()
+    {
+        ok = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const bool good = (uint32_t)page[k] < pages;
+            ok |= good ? 1u << k : 0u;
+            row[k] = (good ? (uint32_t)page[k] * page_ld + (uint32_t)off[k] : 0u) + head;
+            const int o = off[k] + rest, over = o >= page_size ? 1 : 0;
+            off[k] = o - (over ? page_size : 0);
+            j[k] += jump + over;
+        }
+        ask();
+    }
+};
+
 template <int D> struct StreamShape {
     static constexpr int W = D / 32;                       // words of a Key row per lane (four lanes to a row)
     static constexpr int VW = D == 256 ? 2 : 1;            // words of a Value row per lane (16 lanes to a row)
@@ -232,56 +296,28 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
             rowc[x] = fabsf(p.a.scale_log2) * 0x1p20f / power;
         }
 
-        // ---- the tiles' pages
-        int page_j[4], page_off[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int tok = t0 + wave * 64 + 16 * k;
-            page_j[k] = tok / c.page_size;
-            page_off[k] = tok - page_j[k] * c.page_size;
-        }
-        const int32_t *table = t.table + b * t.table_ld;
-        int32_t page[4];
-        auto ask_pages = [&]() {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) page[k] = table[min(page_j[k], t.table_cols - 1)];
-        };
-        int64_t row[4];
-        uint32_t ok = 0, ok_next = 0;
-        auto place_rows = [&]() {                           // (blocks past the table are past every row's limit too)
-            ok_next = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool good = page[k] >= 0 && page[k] < c.pages;
-                ok_next |= good ? 1u << k : 0u;
-                row[k] = (good ? page[k] * c.page_ld + page_off[k] : 0) + h * c.head_ld;
-                page_j[k] += p.page_jump;
-                page_off[k] += p.page_rest;
-                if (page_off[k] >= c.page_size) {
-                    page_off[k] -= c.page_size;
-                    ++page_j[k];
-                }
-            }
-        };
+        TileRows rows(c, t, b, h, t0 + wave * 64, p.page_jump, p.page_rest);
+        uint32_t ok = 0;
 
         // ---- raw rows
         uint32_t kraw[4][W], vraw[4][4][VW];
         int32_t kz[4];
         v4i vw[4], skw[NB], svw[NB];
         const int sgrp = col / RP;                          // lane's copy of the rows: blocks sgrp, sgrp + 16 / RP, ..
+        auto own_block = [&](int n) {                       // the row of a lane's n-th block
+            return NB == 4 ? rows.row[n] : NB == 2 ? pick2(rows.row[2 * n & 3], rows.row[(2 * n + 1) & 3], sgrp) : pick4(rows.row[0], rows.row[1], rows.row[2], rows.row[3], sgrp);
+        };
         auto load_k = [&]() {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[0] + row[k] * (D / 2) + col * (D / 2) + kg * (D / 8));
+                const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[0] + (uint64_t)rows.row[k] * (D / 2) + (uint32_t)(col * (D / 2) + kg * (D / 8)));
 #pragma unroll
                 for (int j = 0; j < W; ++j) kraw[k][j] = src[j];
-                kz[k] = (c.words[0] + row[k])[col];
+                kz[k] = (c.words[0] + rows.row[k])[col];
             }
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                int64_t at = row[n * (4 / NB)];
-#pragma unroll
-                for (int k = 1; k < 4 / NB; ++k) at = sgrp == k ? row[n * (4 / NB) + k] : at;
+                const uint32_t at = own_block(n);
                 skw[n] = *reinterpret_cast<const v4i *>(c.words[0] + at + 4 * kg);
             }
         };
@@ -289,32 +325,28 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
             const int word = Shape::HALVES ? col & 7 : D == 96 ? min(col, 11) : VW * col;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const uint8_t *src = c.packed[1] + row[k] * (D / 2) + 4 * kg * (D / 2) + 4 * word;
+                const uint8_t *src = c.packed[1] + (uint64_t)rows.row[k] * (D / 2) + (uint32_t)(4 * kg * (D / 2) + 4 * word);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
                     for (int v = 0; v < VW; ++v) vraw[k][r][v] = reinterpret_cast<const uint32_t *>(src + r * (D / 2))[v];
-                vw[k] = *reinterpret_cast<const v4i *>(c.words[1] + row[k] + 4 * kg);
+                vw[k] = *reinterpret_cast<const v4i *>(c.words[1] + rows.row[k] + 4 * kg);
             }
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 if (NB == 4) {
                     svw[n] = vw[n];
                 } else {
-                    int64_t at = row[n * (4 / NB)];
-#pragma unroll
-                    for (int k = 1; k < 4 / NB; ++k) at = sgrp == k ? row[n * (4 / NB) + k] : at;
+                    const uint32_t at = own_block(n);
                     svw[n] = *reinterpret_cast<const v4i *>(c.words[1] + at + 4 * kg);
                 }
             }
         };
 
-        ask_pages();
-        place_rows();
+        rows.next();
         load_k();
         load_v();
-        ask_pages();
-        ok = ok_next;
+        ok = rows.ok;
 
         for (int tok = t0 + wave * 64; tok < t1; tok += NW * 64) {
             const bool more = tok + NW * 64 < t1;
@@ -352,7 +384,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
             }
             const bool whole = ok == 15u && tok + 64 <= lim_lo;
             if (more) {
-                place_rows();
+                rows.next();
                 load_k();
             }
             // ---- softmax
@@ -489,8 +521,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
             }
             if (more) {
                 load_v();
-                ask_pages();
-                ok = ok_next;
+                ok = rows.ok;
             }
         }
     }
@@ -652,41 +683,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
         }
 
         // ---- the tiles' rows
-        const int32_t *table = t.table + b * t.table_ld;
-        int page_j[4], page_off[4];
-        int32_t page[4];
-        int64_t row[4];
-        uint32_t ok = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            page_j[k] = (t0 + 16 * k) / c.page_size;
-            page_off[k] = t0 + 16 * k - page_j[k] * c.page_size;
-        }
-        auto ask_pages = [&]() {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) page[k] = table[min(page_j[k], t.table_cols - 1)];
-        };
-        auto place_rows = [&]() {                           // (blocks past the table are past every row's limit too)
-            ok = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool good = page[k] >= 0 && page[k] < c.pages;
-                ok |= good ? 1u << k : 0u;
-                row[k] = (good ? page[k] * c.page_ld + page_off[k] : 0) + h * c.head_ld;
-                page_j[k] += p.page_jump;
-                page_off[k] += p.page_rest;
-                if (page_off[k] >= c.page_size) {
-                    page_off[k] -= c.page_size;
-                    ++page_j[k];
-                }
-            }
-        };
-        auto block_row = [&](int blk) {                     // row of a lane's own block of 16 tokens
-            int64_t at = row[0];
-#pragma unroll
-            for (int k = 1; k < 4; ++k) at = blk == k ? row[k] : at;
-            return at;
-        };
+        TileRows rows(c, t, b, h, t0, p.page_jump, p.page_rest);
+        auto block_row = [&](int blk) { return pick4(rows.row[0], rows.row[1], rows.row[2], rows.row[3], blk); };
         // what this thread decodes of the next tile, as it comes from memory
         const bool keys = wave < NW / 2;
         const int part = keys ? tid : tid - HALF;
@@ -699,16 +697,16 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 #pragma unroll
                 for (int k = 0; k < KT; ++k) {
                     const int w = min(part + k * HALF, 64 * WORDS - 1), tk = w / WORDS;
-                    const int64_t at = block_row(tk >> 4) + (tk & 15);
-                    raw[k] = reinterpret_cast<const uint32_t *>(c.packed[0])[at * WORDS + (w - tk * WORDS)];
+                    const uint32_t at = block_row(tk >> 4) + (tk & 15);
+                    raw[k] = reinterpret_cast<const uint32_t *>(c.packed[0])[(uint64_t)at * WORDS + (w - tk * WORDS)];
                     rw[k] = c.words[0][at];
                 }
             } else {
 #pragma unroll
                 for (int k = 0; k < VT; ++k) {
                     const int w = min(part + k * HALF, 16 * WORDS - 1), tq = w / WORDS;
-                    const int64_t at = block_row(tq >> 2) + 4 * (tq & 3);
-                    const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[1]) + at * WORDS + (w - tq * WORDS);
+                    const uint32_t at = block_row(tq >> 2) + 4 * (tq & 3);
+                    const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[1]) + (uint64_t)at * WORDS + (w - tq * WORDS);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) raw[4 * k + r] = src[r * WORDS];
                     const v4i z = *reinterpret_cast<const v4i *>(c.words[1] + at);
@@ -720,10 +718,10 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb) {
                 const int tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
-                const int64_t at = (i & 8 ? row[2 * tb + 1] : row[2 * tb]) + (tk & 15);
+                const uint32_t at = pick2(rows.row[2 * tb], rows.row[2 * tb + 1], i >> 3) + (tk & 15);
                 stw[tb][0] = c.words[0][at];
                 stw[tb][1] = c.words[1][at];
-                tile_ok[tb] = tok + tk < t1 && (ok >> (2 * tb + (i >> 3)) & 1u);
+                tile_ok[tb] = tok + tk < t1 && (rows.ok >> (2 * tb + (i >> 3)) & 1u);
             }
         };
         auto decode_tile = [&](uint8_t *buf) {
@@ -768,16 +766,14 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
             }
         };
 
-        ask_pages();
-        place_rows();
+        rows.next();
         load_tile(t0);
-        ask_pages();
         int buf = 0;
         for (int tok = t0; tok < t1; tok += 64) {
             uint8_t *lds = tile_lds + buf * BUF;
             buf ^= 1;
             decode_tile(lds);
-            const uint32_t ok_now = ok;
+            const uint32_t ok_now = rows.ok;
             float sk[2], sv[2];
             uint32_t top_step = 0;
 #pragma unroll
@@ -787,9 +783,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
                 top_step = max(top_step, __float_as_uint(sv[tb]));
             }
             if (tok + 64 < t1) {
-                place_rows();
+                rows.next();
                 load_tile(tok + 64);
-                ask_pages();
             }
             __syncthreads();        // (one barrier a tile: the other buffer's readers are behind the last one)
             if (tok >= lim_hi) continue;
@@ -993,7 +988,8 @@ static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, in
     AttnPlan n = {};
     n.splits = 1;
     const int64_t rows = (int64_t)t.S * (Hq / c.heads);
-    const bool pages = c.page_size % 16 == 0 && c.page_ld % 16 == 0 && c.head_ld % 16 == 0 && c.pages > 0 && t.table_cols > 0;
+    const bool pages = c.page_ld < 1LL << 32 && c.head_ld < 1LL << 32 && c.page_size % 16 == 0 && c.page_ld % 16 == 0 && c.head_ld % 16 == 0 && c.pages > 0 && t.table_cols > 0 &&
+                       (c.pages - 1) * c.page_ld + (c.heads - 1) * c.head_ld + c.page_size < 1LL << 32;
     if (dtype == W4A8_F32 || !pages || (c.D != 64 && c.D != 96 && c.D != 128 && c.D != 256)) return n;
     if (rows > 0x7fffffffLL / 2) return n;
     const int64_t tokens = std::max<int64_t>(1, std::min<int64_t>(max_len, (int64_t)t.table_cols * c.page_size));
