@@ -96,12 +96,12 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs p, KvView c, Kv
 // Values it is taken off before the product (one packed subtraction for two): a token with nearly all of the weight would otherwise
 // leave 2^-20 of 16 z + 8 in channels that are zero.  Queries enter as fp16 as they are (bf16: times a power of two per row, so that nothing is lost); the softmax's weights
 // enter as fp16 numbers p step 2^(12 - E), E the exponent of the largest step so far: their rounding to 11 bits is the only one on
-// the way, 2^26 below the largest p step they still have all of them, and 2^37 below it they end.
+// the way, 2^24 below the largest p step they still have all of them, and 2^35 below it they end.
 //
 // A wave takes 64 tokens at a time, alone: scores as (16 tokens) x (16 rows) tiles leave in each lane four tokens of one
 // row, which is what the product with the Values (tokens as the inner dimension, 16 channels x 16 rows out) wants as its
 // operand, so nothing moves between lanes.  With at most 8 (4) rows the 16 columns hold them twice (four times), and each copy
-// does the softmax of another block of 16 tokens.  The running maximum moves only when a score passes it by 2^2.
+// does the softmax of another block of 16 tokens.
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef float v2f __attribute__((ext_vector_type(2)));
@@ -115,8 +115,11 @@ struct StreamArgs {
 };
 
 constexpr float KV_NONE = -1e30f;      // the maximum of no scores
-constexpr float KV_MASKED = -3e38f;
-constexpr float KV_SLACK = 2.0f;       // log2 of what a p may pass the running maximum by
+constexpr float KV_MASKED = -INFINITY; // (times a row's factor, which is not zero)
+constexpr float KV_LEAST = 1.1754943508222875e-38f;
+// The running maximum M moves when a score passes it by 2^2, and then to 2^2 above the new one: scores have to grow by 2^4 before the next
+// move, which 32 rows over some 30 tiles do a few times (with 2^2 alone, in most of the tiles: 139 us for 118).
+constexpr float KV_SLACK = 2.0f, KV_AHEAD = 2.0f;
 
 __device__ __forceinline__ uint32_t kv_lut_hi(int32_t word) { return ((uint32_t)word << 28) | 0x00C8A888u; }
 constexpr uint32_t KV_LUT_LO = 0x68482808u;
@@ -157,6 +160,27 @@ template <> __device__ __forceinline__ float q_power<bf16_t>(float top)
 // kernel writes it), rows are numbered in 32 bits (the launcher checks that the cache has no more).
 typedef const __attribute__((address_space(4))) int32_t *scalar_i32;
 __device__ __forceinline__ scalar_i32 scalar_table(const int32_t *p) { return (scalar_i32)(uintptr_t)p; }
+
+// maxima with the lanes 16 and 32 away, by the swaps of half rows and half waves; and over the wave
+__device__ __forceinline__ float max_xor16(float v)
+{
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float max_xor32(float v)
+{
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
+{
+    v = max(v, (uint32_t)dpp_i32<DPP_QUAD_XOR1>((int)v));
+    v = max(v, (uint32_t)dpp_i32<DPP_QUAD_XOR2>((int)v));
+    v = max(v, (uint32_t)dpp_i32<DPP_ROW_HALF_MIRROR>((int)v));
+    v = max(v, (uint32_t)dpp_i32<DPP_ROW_MIRROR>((int)v));
+    const auto lane = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+    return max(max(lane(0), lane(16)), max(lane(32), lane(48)));
+}
 
 // one of four values by a lane's own index (by value: a choice among array elements would send the array to memory)
 __device__ __forceinline__ uint32_t pick4(uint32_t a, uint32_t b, uint32_t c, uint32_t d, int k)
@@ -293,7 +317,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
             sum += __shfl_xor(sum, 32);
             q16[x] = -sum * 0x1p-20f;                       // -16 units of every token's zero-point
             q8[x] = -sum * 0x1p-21f;
-            rowc[x] = fabsf(p.a.scale_log2) * 0x1p20f / power;
+            rowc[x] = fmaxf(fabsf(p.a.scale_log2) * 0x1p20f / power, KV_LEAST);
         }
 
         TileRows rows(c, t, b, h, t0 + wave * 64, p.page_jump, p.page_rest);
@@ -388,29 +412,34 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
                 load_k();
             }
             // ---- softmax
-            uint32_t live = ~0u;                            // bit 4 n + r of each x in turn
             if (!whole) {
-                live = 0;
+                uint32_t seen[NB][4];                       // (a token that no row sees may hold anything: its step is not used)
 #pragma unroll
-                for (int x = 0; x < RT; ++x)
+                for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int n = 0; n < NB; ++n)
+                    for (int r = 0; r < 4; ++r) {
+                        const int k = n * (4 / NB) + (NB == 4 ? 0 : sgrp);
+                        bool any = false;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int k = n * (4 / NB) + (NB == 4 ? 0 : sgrp);
+                        for (int x = 0; x < RT; ++x) {
                             const bool in = tok + 16 * k + 4 * kg + r < lim[x] && (ok >> k & 1u);
-                            live |= in ? 1u << (x * 16 + 4 * n + r) : 0u;
                             y[x][n][r] = in ? y[x][n][r] : KV_MASKED;
+                            any = any || in;
                         }
+                        seen[n][r] = any ? (uint32_t)svw[n][r] : 0u;
+                    }
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) svw[n][r] = (int)seen[n][r];
             }
-            const uint32_t any_row = RT > 1 ? live | live >> 16 : live;
+            float top[RT];
             uint32_t top_step = 0;
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) top_step = max(top_step, (any_row >> (4 * n + r) & 1u) ? (uint32_t)svw[n][r] & 0x7fffffffu : 0u);
-            bool move = (int)(top_step >> 23) - 127 > E;
-            float top[RT];
+                for (int r = 0; r < 4; ++r) top_step = max(top_step, (uint32_t)svw[n][r] & 0x7fffffffu);
+            bool move = false;
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
                 top[x] = y[x][0][0];
@@ -421,23 +450,28 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
                 top[x] *= rowc[x];
                 move = move || top[x] > M[x] + KV_SLACK;
             }
-            if (__builtin_amdgcn_ballot_w64(move)) {        // rare: another maximum, or a larger step
-                uint32_t e = top_step >> 23;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) e = max(e, (uint32_t)__shfl_xor((int)e, d));
-                const int E_new = max(E, (int)e - 127);
+            if (__builtin_amdgcn_ballot_w64((int)(top_step >> 23) - 127 > E)) {   // rare: a larger step
+                const int E_new = max(E, (int)wave_max_u32(top_step >> 23) - 127);
                 const float shift = __builtin_ldexpf(1.0f, E - E_new);
-                E = __builtin_amdgcn_readfirstlane(E_new);
+                E = E_new;
+#pragma unroll
+                for (int x = 0; x < RT; ++x)
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j) acc[x][j] *= shift;
+            }
+            if (__builtin_amdgcn_ballot_w64(move)) {        // rare: larger scores
 #pragma unroll
                 for (int x = 0; x < RT; ++x) {
-                    float m = fmaxf(top[x], M[x]);
-#pragma unroll
-                    for (int d = RP; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+                    float m = fmaxf(top[x], M[x] - KV_AHEAD);
+                    m = max_xor32(max_xor16(m));
+                    if (RP <= 8) m = fmaxf(m, dpp_f32<DPP_ROW_ROR8>(m));
+                    if (RP <= 4) m = fmaxf(m, dpp_f32<DPP_ROW_ROR4>(m));
+                    m = m > M[x] - KV_AHEAD ? m + KV_AHEAD : M[x];
                     const float keep = __builtin_amdgcn_exp2f(M[x] - m);
                     M[x] = m;
                     l[x] *= keep;
 #pragma unroll
-                    for (int j = 0; j < NJ; ++j) acc[x][j] *= keep * shift;
+                    for (int j = 0; j < NJ; ++j) acc[x][j] *= keep;
                 }
             }
             const float unit = __builtin_ldexpf(1.0f, 12 - E);
@@ -449,13 +483,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
                     float wv[4];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[x][n][r], rowc[x], -M[x]));
+                        const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[x][n][r], rowc[x], -M[x]));
                         wv[r] = pr * (__int_as_float(svw[n][r] & -16) * unit);
-                        if (!whole) {
-                            const bool in = live >> (x * 16 + 4 * n + r) & 1u;
-                            pr = in ? pr : 0.0f;
-                            wv[r] = in ? wv[r] : 0.0f;
-                        }
                         l[x] += pr;
                     }
 #pragma unroll
@@ -679,7 +708,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     q[j][i] = (_Float16)(to_f32(__builtin_bit_cast(T, (uint16_t)(raw[j][i / 2] >> (i & 1) * 16))) * turn);
-            rowc = fabsf(p.a.scale_log2) * 0x1p20f / power;
+            rowc = fmaxf(fabsf(p.a.scale_log2) * 0x1p20f / power, KV_LEAST);
         }
 
         // ---- the tiles' rows
@@ -789,20 +818,19 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
             __syncthreads();        // (one barrier a tile: the other buffer's readers are behind the last one)
             if (tok >= lim_hi) continue;
             const bool whole = ok_now == 15u && tok + 64 <= lim_lo;
-
             v16f y[2];
 #pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
+            for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) y[tb][i] = 0.0f;
 #pragma unroll
-                for (int j = 0; j < KS; ++j) {
+            for (int j = 0; j < KS; ++j)
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) {
                     const v8h a = *reinterpret_cast<const v8h *>(lds + (tb * 32 + col) * KLD + j * 32 + kg * 16);
                     y[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[j], y[tb], 0, 0, 0);
                 }
-            }
             float top = KV_MASKED;
-            uint32_t live = ~0u;
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb)
                 unroll16(std::make_integer_sequence<int, 16>(), [&](auto ic) {
@@ -810,15 +838,12 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
                     y[tb][i] *= row_bcast<i>(sk[tb]);
                 });
             if (!whole) {
-                live = 0;
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
-                        const bool in = tok + tk < lim && (ok_now >> (2 * tb + (i >> 3)) & 1u);
-                        live |= in ? 1u << (tb * 16 + i) : 0u;
-                        y[tb][i] = in ? y[tb][i] : KV_MASKED;
+                        y[tb][i] = tok + tk < lim && (ok_now >> (2 * tb + (i >> 3)) & 1u) ? y[tb][i] : KV_MASKED;
                     }
             }
 #pragma unroll
@@ -826,22 +851,25 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, y[tb][i]);
             top *= rowc;
-            const bool move = (int)(top_step >> 23) - 127 > E || top > M + KV_SLACK;
-            if (__builtin_amdgcn_ballot_w64(move)) {        // rare: another maximum, or a larger step
-                uint32_t e = top_step >> 23;
+            if (__builtin_amdgcn_ballot_w64((int)(top_step >> 23) - 127 > E)) {   // rare: a larger step
+                const int E_new = max(E, (int)wave_max_u32(top_step >> 23) - 127);
+                const float shift = __builtin_ldexpf(1.0f, E - E_new);
+                E = E_new;
 #pragma unroll
-                for (int d = 1; d < 64; d <<= 1) e = max(e, (uint32_t)__shfl_xor((int)e, d));
-                const int E_new = max(E, (int)e - 127);
-                float m = fmaxf(top, M);
-                m = fmaxf(m, __shfl_xor(m, 32));
-                const float keep = __builtin_amdgcn_exp2f(M - m), both = __builtin_ldexpf(keep, E - E_new);
-                E = __builtin_amdgcn_readfirstlane(E_new);
+                for (int k = 0; k < CB; ++k)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[k][i] *= shift;
+            }
+            if (__builtin_amdgcn_ballot_w64(top > M + KV_SLACK)) {                // rare: larger scores
+                float m = max_xor32(fmaxf(top, M - KV_AHEAD));
+                m = m > M - KV_AHEAD ? m + KV_AHEAD : M;
+                const float keep = __builtin_amdgcn_exp2f(M - m);
                 M = m;
                 l *= keep;
 #pragma unroll
                 for (int k = 0; k < CB; ++k)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[k][i] *= both;
+                    for (int i = 0; i < 16; ++i) acc[k][i] *= keep;
             }
             const float unit = __builtin_ldexpf(1.0f, 12 - E);
             v4u w[4];
@@ -851,8 +879,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
                 float wv[16];
                 unroll16(std::make_integer_sequence<int, 16>(), [&](auto ic) {
                     constexpr int i = decltype(ic)::value;
-                    float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[tb][i], rowc, -M));
-                    if (!whole) pr = live >> (tb * 16 + i) & 1u ? pr : 0.0f;
+                    const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[tb][i], rowc, -M));
                     l += pr;
                     wv[i] = pr * row_bcast<i>(svn);
                 });
