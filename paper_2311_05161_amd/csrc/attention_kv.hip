@@ -258,11 +258,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, kg = lane >> 4;
     int id = blockIdx.x;
-    const int split = id % p.splits;
-    id /= p.splits;
     const int rt = id % p.row_tiles;
     id /= p.row_tiles;
-    const int h = id % c.heads, b = id / c.heads;
+    const int h = id % c.heads;
+    id /= c.heads;
+    const int b = id % t.B, split = id / t.B;
     const int group = p.a.group, row0 = rt * ROWS;
     const KvLength len = kv_length(t, c, b);
 
@@ -648,6 +648,8 @@ __device__ __forceinline__ v4u kv_halves(uint32_t p, int32_t word)
 // 16 channels eight apart (the decoder's writes) meet in a bank more often than they must
 __device__ __forceinline__ int v_chunk(int ch, int chunk) { return chunk ^ (((ch >> 1) ^ (ch >> 3)) & 7); }
 
+constexpr int TILE_RUN = 4;
+
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p, KvView c, KvTokens t)
 {
@@ -662,8 +664,15 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
     int id = blockIdx.x;
     const int split = id % p.splits;
     id /= p.splits;
-    const int bh = id % (t.B * c.heads), rt = p.row_tiles - 1 - id / (t.B * c.heads);   // (longest first)
-    const int h = bh % c.heads, b = bh / c.heads;
+    // longest tiles first, and the row tiles of a (sequence, head) in runs of TILE_RUN: workgroups go to an XCD's four shader engines in
+    // turn whether these are busy or not, so a period of 2 or 4 in what they have to do would leave engines idle (two sequences of
+    // 3000 and 743 tokens, the short one's empty workgroups every second place: 226 us; in runs 160)
+    const int h = id % c.heads;
+    id /= c.heads;
+    const int run = min(TILE_RUN, p.row_tiles), in_run = id % run;
+    id /= run;
+    const int b = id % t.B, rt = p.row_tiles - 1 - (id / t.B * run + in_run);
+    if (rt < 0) return;
     const int group = p.a.group, row0 = rt * NW * 32, wrow0 = row0 + wave * 32;
     const KvLength len = kv_length(t, c, b);
     auto limit = [&](int r) { return min(len.start + r / group + 1, p.a.max_len); };    // tokens that a row sees, if it is there
@@ -795,6 +804,10 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
             }
         };
 
+        int v_off[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) v_off[s] = col * 128 + v_chunk(col, 2 * s + kg) * 16;
+        if (wave < NW / 2) __builtin_amdgcn_s_setprio(1);
         rows.next();
         load_tile(t0);
         int buf = 0;
@@ -838,6 +851,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
                     y[tb][i] *= row_bcast<i>(sk[tb]);
                 });
             if (!whole) {
+                asm volatile("");                           // (keeps this a branch: as selects it would be done for every tile)
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
@@ -890,9 +904,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
-                for (int k = 0; k < CB; ++k) {
-                    const int ch = k * 32 + col;
-                    const v8h a = *reinterpret_cast<const v8h *>(lds + KBYTES + ch * 128 + v_chunk(ch, 2 * s + kg) * 16);
+                for (int k = 0; k < CB; ++k) {              // (32 channels on, the chunk's third bit is the other one)
+                    const v8h a = *reinterpret_cast<const v8h *>(lds + KBYTES + v_off[s ^ (k & 1) * 2] + k * 4096);
                     acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(v8h, w[s]), acc[k], 0, 0, 0);
                 }
         }
@@ -937,48 +950,74 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
     }
 }
 
-// Joins the splits: a workgroup per (sequence, head, row)
+// Joins the splits.  A group of D / 4 lanes has four channels each of a row and a share of its splits: `ways` groups per row, their
+// sums meet in LDS.  Reads every part once; few splits (many rows): a group does a whole row, with its loads all in flight.
 template <typename T>
-__global__ __launch_bounds__(256) void attn_join_kernel(StreamArgs p, int heads, int S, int D)
+__global__ __launch_bounds__(256) void attn_join_kernel(StreamArgs p, int heads, int S, int D, int ways, int64_t all_rows)
 {
     __shared__ float red[5][256];
-    const int64_t at = blockIdx.x;
-    const int rr = (int)(at % p.rows);
-    const int64_t bh = at / p.rows;
-    const int h = (int)(bh % heads), tid = threadIdx.x;
-    const int64_t b = bh / heads;
-    const float *ml = p.part_ml + at * p.splits * 2, *po = p.part_o + at * p.splits * D;
-    float m = KV_NONE;
-    for (int s = tid & 63; s < p.splits; s += 64) m = ml[2 * s + 1] > 0.0f ? fmaxf(m, ml[2 * s]) : m;
-    m = wave_max(m);
-    const int s0 = rr / p.a.group;
-    const int64_t out = (b * S + s0) * p.a.Hq + h * p.a.group + (rr - s0 * p.a.group);
-    const int quad = D / 4, ways = 256 / quad, way = tid / quad, ch = (tid - way * quad) * 4;
-    float sum = 0.0f;
+    const int quad = D / 4, groups = 256 / quad, per = groups / ways;
+    const int g = threadIdx.x / quad, ch = (threadIdx.x - g * quad) * 4, way = g / per;
+    const int64_t at = (int64_t)blockIdx.x * per + (g - way * per);
+    const bool mine = way < ways && at < all_rows;
+    const float *ml = p.part_ml + at * p.splits * 2, *po = p.part_o + at * p.splits * D + ch;
+    // every lane looks over all maxima of its row (they are few, and in cache after the first), so the groups agree on it
+    float m = KV_NONE, sum = 0.0f;
     v4f o = {0, 0, 0, 0};
-    if (way < ways) {
+    if (mine) {
+        for (int s = 0; s < p.splits; ++s) {
+            const v2f x = *reinterpret_cast<const v2f *>(ml + 2 * s);
+            m = x[1] > 0.0f ? fmaxf(m, x[0]) : m;
+        }
+#pragma unroll 4
         for (int s = way; s < p.splits; s += ways) {
-            const float ls = ml[2 * s + 1];
-            if (ls > 0.0f) {
-                const float f = __builtin_amdgcn_exp2f(ml[2 * s] - m);
-                sum += f * ls;
-                o += *reinterpret_cast<const v4f *>(po + (int64_t)s * D + ch) * f;
+            const v2f x = *reinterpret_cast<const v2f *>(ml + 2 * s);
+            if (x[1] > 0.0f) {                              // (a part without tokens was not written)
+                const float f = __builtin_amdgcn_exp2f(x[0] - m);
+                sum += f * x[1];
+                o += *reinterpret_cast<const v4f *>(po + (int64_t)s * D) * f;
             }
         }
     }
+    if (ways > 1) {                                         // (uniform)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) red[i][tid] = o[i];
-    red[4][tid] = sum;
-    __syncthreads();
-    if (tid < quad) {
-        for (int w = 1; w < ways; ++w) {
+        for (int i = 0; i < 4; ++i) red[i][threadIdx.x] = o[i];
+        red[4][threadIdx.x] = sum;
+        __syncthreads();
+        if (mine && way == 0) {
+            for (int w = 1; w < ways; ++w) {
+                const int from = threadIdx.x + w * per * quad;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += red[i][tid + w * quad];
-            sum += red[4][tid + w * quad];
+                for (int i = 0; i < 4; ++i) o[i] += red[i][from];
+                sum += red[4][from];
+            }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ((T *)p.a.out)[out * D + ch + i] = attn_from_f32<T>(sum > 0.0f ? o[i] / sum : 0.0f);
     }
+    if (mine && way == 0) {
+        const int rr = (int)(at % p.rows);
+        const int64_t bh = at / p.rows, b = bh / heads;
+        const int h = (int)(bh - b * heads), s = rr / p.a.group;
+        T *out = (T *)p.a.out + ((b * S + s) * p.a.Hq + h * p.a.group + (rr - s * p.a.group)) * D + ch;
+        uint16_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint16_t, attn_from_f32<T>(sum > 0.0f ? o[i] / sum : 0.0f));
+        *reinterpret_cast<v2u *>(out) = v2u{(uint32_t)r[0] | (uint32_t)r[1] << 16, (uint32_t)r[2] | (uint32_t)r[3] << 16};
+    }
+}
+
+template <typename T>
+static int launch_join(const StreamArgs &p, const KvView &c, const KvTokens &t, hipStream_t st)
+{
+    if (p.splits > 1) {
+        const int64_t rows = (int64_t)t.B * c.heads * p.rows;
+        const int groups = 256 / (c.D / 4);
+        int ways = 1;
+        while (ways * 2 <= groups && ways * 4 <= p.splits) ways *= 2;
+        const int64_t per = groups / ways, blocks = (rows + per - 1) / per;
+        if (blocks > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+        hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, st, p, c.heads, t.S, c.D, ways, rows);
+    }
+    return hip_status(hipGetLastError());
 }
 
 template <typename T>
@@ -1065,9 +1104,7 @@ static int launch_stream(const StreamArgs &p, const KvView &c, const KvTokens &t
     const int64_t blocks = (int64_t)t.B * c.heads * p.row_tiles * p.splits;
     if (blocks > 0x7fffffffLL) return W4A8_ERR_SHAPE;
     hipLaunchKernelGGL((attn_stream_kernel<T, D, RP, RT, NW>), dim3((unsigned)blocks), dim3(NW * 64), bytes, st, p, c, t);
-    if (p.splits > 1)
-        hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)((int64_t)t.B * c.heads * p.rows)), dim3(256), 0, st, p, c.heads, t.S, c.D);
-    return hip_status(hipGetLastError());
+    return launch_join<T>(p, c, t, st);
 }
 
 template <typename T, int D, int NW>
@@ -1079,11 +1116,11 @@ static int launch_tile(const StreamArgs &p, const KvView &c, const KvTokens &t, 
         const int rc = opt_in_dynamic_lds((const void *)attn_tile_kernel<T, D, NW>, bytes, done);
         if (rc != W4A8_OK) return rc;
     }
-    const int64_t blocks = (int64_t)t.B * c.heads * p.row_tiles * p.splits, joins = (int64_t)t.B * c.heads * p.rows;
-    if (blocks > 0x7fffffffLL || joins > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+    const int64_t run = std::min(TILE_RUN, p.row_tiles);
+    const int64_t blocks = (int64_t)t.B * c.heads * ((p.row_tiles + run - 1) / run * run) * p.splits;
+    if (blocks > 0x7fffffffLL) return W4A8_ERR_SHAPE;
     hipLaunchKernelGGL((attn_tile_kernel<T, D, NW>), dim3((unsigned)blocks), dim3(NW * 64), bytes, st, p, c, t);
-    if (p.splits > 1) hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)joins), dim3(256), 0, st, p, c.heads, t.S, c.D);
-    return hip_status(hipGetLastError());
+    return launch_join<T>(p, c, t, st);
 }
 
 template <typename T, int D>
