@@ -655,9 +655,10 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 {
     constexpr int KLD = D * 2 + 16, KBYTES = 64 * KLD, VBYTES = D * 128, BUF = KBYTES + VBYTES;
     constexpr int KS = D / 16, CB = D / 32, WORDS = D / 8;
-    constexpr int HALF = NW / 2 * 64;                       // threads that decode Keys; as many decode Values
-    constexpr int KT = (64 * WORDS + HALF - 1) / HALF;      // words per thread (Keys)
-    constexpr int VT = (16 * WORDS + HALF - 1) / HALF;      // words of four tokens per thread (Values)
+    constexpr int PW = D == 96 ? 16 : WORDS, TPL = 64 / PW; // lanes to a row, rows to a wave's load
+    constexpr int DW = NW / 2, BLOCKS = 4 / DW;             // waves that decode Keys (as many decode Values), blocks of 16 tokens for each
+    constexpr int KT = 16 / TPL, VT = TPL >= 4 ? 1 : 4 / TPL;   // words per lane and block: of Keys; of four tokens' Values
+    constexpr int RAW = BLOCKS * (KT > 4 * VT ? KT : 4 * VT);
     extern __shared__ uint8_t tile_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, kg = lane >> 5;
@@ -722,71 +723,66 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 
         // ---- the tiles' rows
         TileRows rows(c, t, b, h, t0, p.page_jump, p.page_rest);
-        auto block_row = [&](int blk) { return pick4(rows.row[0], rows.row[1], rows.row[2], rows.row[3], blk); };
-        // what this thread decodes of the next tile, as it comes from memory
-        const bool keys = wave < NW / 2;
-        const int part = keys ? tid : tid - HALF;
-        uint32_t raw[KT > 4 * VT ? KT : 4 * VT];
-        int32_t rw[KT > 4 * VT ? KT : 4 * VT];
-        int32_t stw[2][2];                                  // words of Keys and Values for the softmax: lane i & 15's token of block 0, 1
-        int tile_ok[2];                                     // which of them count
-        auto load_tile = [&](int tok) {
-            if (keys) {
+        // What this thread decodes, as it comes from memory: a wave has whole blocks of 16 tokens, so a row's address is a scalar and a
+        // lane's constant.
+        const bool keys = wave < DW;
+        const int dwave = keys ? wave : wave - DW, sub = lane / PW, word = min(lane - sub * PW, WORDS - 1);
+        const bool decodes = (PW == WORDS || lane - sub * PW < WORDS) && (keys || sub < 4);
+        uint32_t raw[RAW];
+        int32_t rw[RAW];
+        auto load_raw = [&]() {
 #pragma unroll
-                for (int k = 0; k < KT; ++k) {
-                    const int w = min(part + k * HALF, 64 * WORDS - 1), tk = w / WORDS;
-                    const uint32_t at = block_row(tk >> 4) + (tk & 15);
-                    raw[k] = reinterpret_cast<const uint32_t *>(c.packed[0])[(uint64_t)at * WORDS + (w - tk * WORDS)];
-                    rw[k] = c.words[0][at];
+            for (int n = 0; n < BLOCKS; ++n) {
+                const uint32_t at = pick4(rows.row[0], rows.row[1], rows.row[2], rows.row[3], dwave + DW * n);
+                if (keys) {
+                    const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[0]) + (uint64_t)at * WORDS;
+                    const int32_t *zw = c.words[0] + at;
+#pragma unroll
+                    for (int k = 0; k < KT; ++k) {
+                        raw[n * KT + k] = src[(uint32_t)(sub * WORDS + word) + k * TPL * WORDS];
+                        rw[n * KT + k] = zw[(uint32_t)sub + k * TPL];
+                    }
+                } else {
+                    const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[1]) + (uint64_t)at * WORDS;
+                    const int32_t *zw = c.words[1] + at;
+#pragma unroll
+                    for (int k = 0; k < VT; ++k) {
+                        const uint32_t quad = k * TPL + (TPL > 4 ? sub & 3 : sub);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) raw[4 * (n * VT + k) + r] = src[4 * quad * WORDS + word + r * WORDS];
+                        const v4i z = *reinterpret_cast<const v4i *>(zw + 4 * quad);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) rw[4 * (n * VT + k) + r] = z[r];
+                    }
                 }
-            } else {
-#pragma unroll
-                for (int k = 0; k < VT; ++k) {
-                    const int w = min(part + k * HALF, 16 * WORDS - 1), tq = w / WORDS;
-                    const uint32_t at = block_row(tq >> 2) + 4 * (tq & 3);
-                    const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[1]) + (uint64_t)at * WORDS + (w - tq * WORDS);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) raw[4 * k + r] = src[r * WORDS];
-                    const v4i z = *reinterpret_cast<const v4i *>(c.words[1] + at);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) rw[4 * k + r] = z[r];
-                }
-            }
-            const int i = lane & 15;
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
-                const int tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
-                const uint32_t at = pick2(rows.row[2 * tb], rows.row[2 * tb + 1], i >> 3) + (tk & 15);
-                stw[tb][0] = c.words[0][at];
-                stw[tb][1] = c.words[1][at];
-                tile_ok[tb] = tok + tk < t1 && (rows.ok >> (2 * tb + (i >> 3)) & 1u);
             }
         };
-        auto decode_tile = [&](uint8_t *buf) {
-            if (keys) {
+        auto decode_raw = [&](uint8_t *buf) {
 #pragma unroll
-                for (int k = 0; k < KT; ++k) {
-                    const int w = part + k * HALF, tk = w / WORDS;
-                    if (64 * WORDS % HALF == 0 || w < 64 * WORDS)
-                        *reinterpret_cast<v4u *>(buf + tk * KLD + (w - tk * WORDS) * 16) = kv_halves(raw[k], rw[k]);
-                }
-            } else {
+            for (int n = 0; n < BLOCKS; ++n) {
+                const int block = dwave + DW * n;
+                if (keys) {
 #pragma unroll
-                for (int k = 0; k < VT; ++k) {
-                    const int w = part + k * HALF, tq = w / WORDS, m = w - tq * WORDS;
-                    if (16 * WORDS % HALF == 0 || w < 16 * WORDS) {
+                    for (int k = 0; k < KT; ++k) {
+                        const v4u o = kv_halves(raw[n * KT + k], rw[n * KT + k]);
+                        if (decodes) *reinterpret_cast<v4u *>(buf + (16 * block + sub) * KLD + word * 16 + k * TPL * KLD) = o;
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < VT; ++k) {
+                        const int quad = k * TPL + sub, chunk = 2 * block + (quad & 1), off = 8 * (quad >> 1 & 1);
                         uint32_t lo4[4], hi4[4], lut[4];
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            lut[r] = kv_lut_hi(rw[4 * k + r]);
-                            lo4[r] = kv_bytes(raw[4 * k + r], lut[r]);
-                            hi4[r] = kv_bytes(raw[4 * k + r] >> 4, lut[r]);
+                            const uint32_t w = raw[4 * (n * VT + k) + r];
+                            lut[r] = kv_lut_hi(rw[4 * (n * VT + k) + r]);
+                            lo4[r] = kv_bytes(w, lut[r]);
+                            hi4[r] = kv_bytes(w >> 4, lut[r]);
                         }
                         v2h zero[2];
 #pragma unroll
                         for (int r = 0; r < 2; ++r)
                             zero[r] = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(lut[2 * r + 1], lut[2 * r], 0x0c070c03u) | 0x00080008u);
-                        const int chunk = 2 * (tq >> 2) + (tq & 1), off = 8 * ((tq >> 1) & 1);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             const uint32_t sel = 0x0c040c00u + (uint32_t)(j & 3) * 0x00010001u;
@@ -796,41 +792,65 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
                                 const uint32_t two = j < 4 ? __builtin_amdgcn_perm(lo4[2 * r + 1], lo4[2 * r], sel) : __builtin_amdgcn_perm(hi4[2 * r + 1], hi4[2 * r], sel);
                                 o[r] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, two) - zero[r]);
                             }
-                            const int ch = 8 * m + j;
-                            *reinterpret_cast<v2u *>(buf + KBYTES + ch * 128 + v_chunk(ch, chunk) * 16 + off) = o;
+                            const int ch = 8 * word + (j & 6);  // (an odd channel lies in the next row, at the same chunk)
+                            if (decodes) *reinterpret_cast<v2u *>(buf + KBYTES + ch * 128 + v_chunk(ch, chunk) * 16 + off + (j & 1) * 128) = o;
                         }
                     }
                 }
+            }
+        };
+        // the words of Keys and Values for the softmax: lane i & 15's token, in the first and the second 32
+        int32_t stw[2][2];
+        auto load_steps = [&](uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+            const int i = lane & 15;
+#pragma unroll
+            for (int tb = 0; tb < 2; ++tb) {
+                const uint32_t at = pick2(tb ? r2 : r0, tb ? r3 : r1, i >> 3) + (uint32_t)(8 * (i >> 2 & 1) + 4 * kg + (i & 3));
+                stw[tb][0] = c.words[0][at];
+                stw[tb][1] = c.words[1][at];
             }
         };
 
         int v_off[4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) v_off[s] = col * 128 + v_chunk(col, 2 * s + kg) * 16;
-        if (wave < NW / 2) __builtin_amdgcn_s_setprio(1);
         rows.next();
-        load_tile(t0);
+        load_raw();
+        load_steps(rows.row[0], rows.row[1], rows.row[2], rows.row[3]);
+        uint32_t ok_now = rows.ok;
+        decode_raw(tile_lds);
+        rows.next();
+        if (t0 + 64 < t1) load_raw();
         int buf = 0;
         for (int tok = t0; tok < t1; tok += 64) {
-            uint8_t *lds = tile_lds + buf * BUF;
+            // One barrier a tile: behind it this tile is in LDS and the other buffer is free.  The next tile's Values are decoded in front of
+            // this tile's products and its Keys behind them, so that of a SIMD's two waves one has vector work while the other multiplies.
+            __syncthreads();
+            uint8_t *lds = tile_lds + buf * BUF, *other = tile_lds + (buf ^ 1) * BUF;
             buf ^= 1;
-            decode_tile(lds);
-            const uint32_t ok_now = rows.ok;
             float sk[2], sv[2];
             uint32_t top_step = 0;
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb) {
-                sk[tb] = tile_ok[tb] ? kv_step(stw[tb][0]) : 0.0f;
-                sv[tb] = tile_ok[tb] ? fabsf(kv_step(stw[tb][1])) : 0.0f;
+                const int i = lane & 15, tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
+                const bool counts = tok + tk < t1 && (ok_now >> (2 * tb + (i >> 3)) & 1u);
+                sk[tb] = counts ? kv_step(stw[tb][0]) : 0.0f;
+                sv[tb] = counts ? fabsf(kv_step(stw[tb][1])) : 0.0f;
                 top_step = max(top_step, __float_as_uint(sv[tb]));
             }
-            if (tok + 64 < t1) {
-                rows.next();
-                load_tile(tok + 64);
+            const uint32_t ok_tile = ok_now;
+            const bool whole = ok_tile == 15u && tok + 64 <= lim_lo;
+            const bool more = tok + 64 < t1, more2 = tok + 128 < t1;
+            if (more) {
+                load_steps(rows.row[0], rows.row[1], rows.row[2], rows.row[3]);
+                ok_now = rows.ok;
             }
-            __syncthreads();        // (one barrier a tile: the other buffer's readers are behind the last one)
-            if (tok >= lim_hi) continue;
-            const bool whole = ok_now == 15u && tok + 64 <= lim_lo;
+            rows.next();
+            if (!keys) {
+                if (more) decode_raw(other);
+                if (more2) load_raw();
+            }
+            if (tok < lim_hi) {
             v16f y[2];
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb)
@@ -857,7 +877,7 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
-                        y[tb][i] = tok + tk < lim && (ok_now >> (2 * tb + (i >> 3)) & 1u) ? y[tb][i] : KV_MASKED;
+                        y[tb][i] = tok + tk < lim && (ok_tile >> (2 * tb + (i >> 3)) & 1u) ? y[tb][i] : KV_MASKED;
                     }
             }
 #pragma unroll
@@ -908,6 +928,11 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
                     const v8h a = *reinterpret_cast<const v8h *>(lds + KBYTES + v_off[s ^ (k & 1) * 2] + k * 4096);
                     acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(v8h, w[s]), acc[k], 0, 0, 0);
                 }
+            }
+            if (keys) {
+                if (more) decode_raw(other);
+                if (more2) load_raw();
+            }
         }
     }
 
