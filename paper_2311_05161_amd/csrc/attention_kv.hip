@@ -413,6 +413,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
             }
             // ---- softmax
             if (!whole) {
+                int end[RT];                                // (through the statement below, so that this stays a branch)
+#pragma unroll
+                for (int x = 0; x < RT; ++x) {
+                    end[x] = lim[x];
+                    asm volatile("" : "+v"(end[x]));
+                }
                 uint32_t seen[NB][4];                       // (a token that no row sees may hold anything: its step is not used)
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
@@ -422,7 +428,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
                         bool any = false;
 #pragma unroll
                         for (int x = 0; x < RT; ++x) {
-                            const bool in = tok + 16 * k + 4 * kg + r < lim[x] && (ok >> k & 1u);
+                            const bool in = tok + 16 * k + 4 * kg + r < end[x] && (ok >> k & 1u);
                             y[x][n][r] = in ? y[x][n][r] : KV_MASKED;
                             any = any || in;
                         }
@@ -644,9 +650,9 @@ __device__ __forceinline__ v4u kv_halves(uint32_t p, int32_t word)
     return o;
 }
 
-// 16-byte chunk of a channel's row of 64 tokens in LDS: spread so that neither 16 channels in a row (the product's reads) nor
-// 16 channels eight apart (the decoder's writes) meet in a bank more often than they must
-__device__ __forceinline__ int v_chunk(int ch, int chunk) { return chunk ^ (((ch >> 1) ^ (ch >> 3)) & 7); }
+// 16-byte chunk of a channel's row of 64 tokens in LDS: spread so that neither eight channels in a row (the product's reads) nor
+// eight channels eight apart (the decoder's writes) meet in a bank
+__device__ __forceinline__ int v_chunk(int ch, int chunk) { return chunk ^ ((ch ^ (ch >> 3)) & 7); }
 
 constexpr int TILE_RUN = 4;
 
@@ -792,8 +798,8 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
                                 const uint32_t two = j < 4 ? __builtin_amdgcn_perm(lo4[2 * r + 1], lo4[2 * r], sel) : __builtin_amdgcn_perm(hi4[2 * r + 1], hi4[2 * r], sel);
                                 o[r] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, two) - zero[r]);
                             }
-                            const int ch = 8 * word + (j & 6);  // (an odd channel lies in the next row, at the same chunk)
-                            if (decodes) *reinterpret_cast<v2u *>(buf + KBYTES + ch * 128 + v_chunk(ch, chunk) * 16 + off + (j & 1) * 128) = o;
+                            const int ch = 8 * word + j;
+                            if (decodes) *reinterpret_cast<v2u *>(buf + KBYTES + ch * 128 + v_chunk(ch, chunk) * 16 + off) = o;
                         }
                     }
                 }
@@ -851,82 +857,83 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
                 if (more2) load_raw();
             }
             if (tok < lim_hi) {
-            v16f y[2];
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) y[tb][i] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < KS; ++j)
-#pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
-                    const v8h a = *reinterpret_cast<const v8h *>(lds + (tb * 32 + col) * KLD + j * 32 + kg * 16);
-                    y[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[j], y[tb], 0, 0, 0);
-                }
-            float top = KV_MASKED;
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-                unroll16(std::make_integer_sequence<int, 16>(), [&](auto ic) {
-                    constexpr int i = decltype(ic)::value;
-                    y[tb][i] *= row_bcast<i>(sk[tb]);
-                });
-            if (!whole) {
-                asm volatile("");                           // (keeps this a branch: as selects it would be done for every tile)
+                v16f y[2];
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
-                        y[tb][i] = tok + tk < lim && (ok_tile >> (2 * tb + (i >> 3)) & 1u) ? y[tb][i] : KV_MASKED;
+                    for (int i = 0; i < 16; ++i) y[tb][i] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < KS; ++j)
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        const v8h a = *reinterpret_cast<const v8h *>(lds + (tb * 32 + col) * KLD + j * 32 + kg * 16);
+                        y[tb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[j], y[tb], 0, 0, 0);
                     }
-            }
+                float top = KV_MASKED;
 #pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
+                for (int tb = 0; tb < 2; ++tb)
+                    unroll16(std::make_integer_sequence<int, 16>(), [&](auto ic) {
+                        constexpr int i = decltype(ic)::value;
+                        y[tb][i] *= row_bcast<i>(sk[tb]);
+                    });
+                if (!whole) {
+                    int end = lim;                             // (through the statement below, so that this stays a branch: as selects it would
+                    asm volatile("" : "+v"(end));              // be done for every tile)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, y[tb][i]);
-            top *= rowc;
-            if (__builtin_amdgcn_ballot_w64((int)(top_step >> 23) - 127 > E)) {   // rare: a larger step
-                const int E_new = max(E, (int)wave_max_u32(top_step >> 23) - 127);
-                const float shift = __builtin_ldexpf(1.0f, E - E_new);
-                E = E_new;
+                    for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                for (int k = 0; k < CB; ++k)
+                        for (int i = 0; i < 16; ++i) {
+                            const int tk = tb * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
+                            y[tb][i] = tok + tk < end && (ok_tile >> (2 * tb + (i >> 3)) & 1u) ? y[tb][i] : KV_MASKED;
+                        }
+                }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[k][i] *= shift;
-            }
-            if (__builtin_amdgcn_ballot_w64(top > M + KV_SLACK)) {                // rare: larger scores
-                float m = max_xor32(fmaxf(top, M - KV_AHEAD));
-                m = m > M - KV_AHEAD ? m + KV_AHEAD : M;
-                const float keep = __builtin_amdgcn_exp2f(M - m);
-                M = m;
-                l *= keep;
+                for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                for (int k = 0; k < CB; ++k)
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, y[tb][i]);
+                top *= rowc;
+                if (__builtin_amdgcn_ballot_w64((int)(top_step >> 23) - 127 > E)) {   // rare: a larger step
+                    const int E_new = max(E, (int)wave_max_u32(top_step >> 23) - 127);
+                    const float shift = __builtin_ldexpf(1.0f, E - E_new);
+                    E = E_new;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[k][i] *= keep;
-            }
-            const float unit = __builtin_ldexpf(1.0f, 12 - E);
-            v4u w[4];
+                    for (int k = 0; k < CB; ++k)
 #pragma unroll
-            for (int tb = 0; tb < 2; ++tb) {
-                const float svn = sv[tb] * unit;
-                float wv[16];
-                unroll16(std::make_integer_sequence<int, 16>(), [&](auto ic) {
-                    constexpr int i = decltype(ic)::value;
-                    const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[tb][i], rowc, -M));
-                    l += pr;
-                    wv[i] = pr * row_bcast<i>(svn);
-                });
+                        for (int i = 0; i < 16; ++i) acc[k][i] *= shift;
+                }
+                if (__builtin_amdgcn_ballot_w64(top > M + KV_SLACK)) {                // rare: larger scores
+                    float m = max_xor32(fmaxf(top, M - KV_AHEAD));
+                    m = m > M - KV_AHEAD ? m + KV_AHEAD : M;
+                    const float keep = __builtin_amdgcn_exp2f(M - m);
+                    M = m;
+                    l *= keep;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    w[2 * tb + i / 4][i & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{wv[2 * i], wv[2 * i + 1]}), v2h));
-            }
+                    for (int k = 0; k < CB; ++k)
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
+                        for (int i = 0; i < 16; ++i) acc[k][i] *= keep;
+                }
+                const float unit = __builtin_ldexpf(1.0f, 12 - E);
 #pragma unroll
-                for (int k = 0; k < CB; ++k) {              // (32 channels on, the chunk's third bit is the other one)
-                    const v8h a = *reinterpret_cast<const v8h *>(lds + KBYTES + v_off[s ^ (k & 1) * 2] + k * 4096);
-                    acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(v8h, w[s]), acc[k], 0, 0, 0);
+                for (int tb = 0; tb < 2; ++tb) {
+                    const float svn = sv[tb] * unit;
+                    float wv[16];
+                    unroll16(std::make_integer_sequence<int, 16>(), [&](auto ic) {
+                        constexpr int i = decltype(ic)::value;
+                        const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[tb][i], rowc, -M));
+                        l += pr;
+                        wv[i] = pr * row_bcast<i>(svn);
+                    });
+                    v4u w[2];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        w[i / 4][i & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{wv[2 * i], wv[2 * i + 1]}), v2h));
+#pragma unroll
+                    for (int s = 2 * tb; s < 2 * tb + 2; ++s)
+#pragma unroll
+                        for (int k = 0; k < CB; ++k) {      // (32 channels on, the chunk's third bit is the other one)
+                            const v8h a = *reinterpret_cast<const v8h *>(lds + KBYTES + v_off[s ^ (k & 1) * 2] + k * 4096);
+                            acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, __builtin_bit_cast(v8h, w[s & 1]), acc[k], 0, 0, 0);
+                        }
                 }
             }
             if (keys) {
