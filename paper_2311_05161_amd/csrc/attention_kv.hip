@@ -126,7 +126,10 @@ constexpr uint32_t KV_LUT_LO = 0x68482808u;
 // four nibbles (the low ones of p's bytes) -> four bytes n
 __device__ __forceinline__ uint32_t kv_bytes(uint32_t p, uint32_t hi)
 {
-    return __builtin_amdgcn_perm(hi, KV_LUT_LO, p & 0x07070707u) + ((p & 0x08080808u) << 1);
+    // (written out: the compiler turns (p & 8..) << 1 into two instructions and adds with a third)
+    uint32_t n;
+    asm("v_lshl_add_u32 %0, %1, 1, %2" : "=v"(n) : "v"(p & 0x08080808u), "v"(__builtin_amdgcn_perm(hi, KV_LUT_LO, p & 0x07070707u)));
+    return n;
 }
 
 template <typename T> __device__ __forceinline__ void load_q8(const T *p, bool vec, float (&v)[8])
@@ -190,6 +193,16 @@ __device__ __forceinline__ uint32_t pick4(uint32_t a, uint32_t b, uint32_t c, ui
 }
 __device__ __forceinline__ uint32_t pick2(uint32_t a, uint32_t b, int k) { return k & 1 ? b : a; }
 
+// kv_length, from scalar loads; the table has at most 2^30 places here
+__device__ __forceinline__ KvLength scalar_length(const KvTokens &t, const KvView &c, int b)
+{
+    const int room = t.table_cols * c.page_size, count = t.count ? scalar_table(t.count)[b] : t.S;
+    KvLength n;
+    n.start = min(max(scalar_table(t.start)[b], 0), room);
+    n.count = min(min(max(count, 0), t.S), room - n.start);
+    return n;
+}
+
 struct TileRows {
     scalar_i32 table;
     int last, page_size, jump, rest;   // the table's last entry; a tile further is `jump` pages and `rest` tokens
@@ -209,10 +222,13 @@ struct TileRows {
         pages = (uint32_t)c.pages;
         page_ld = (uint32_t)c.page_ld;
         head = (uint32_t)h * (uint32_t)c.head_ld;
+        j[0] = (int)((uint32_t)token / (uint32_t)page_size);
+        off[0] = token - j[0] * page_size;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            j[k] = (int)((uint32_t)(token + 16 * k) / (uint32_t)page_size);
-            off[k] = token + 16 * k - j[k] * page_size;
+        for (int k = 1; k < 4; ++k) {
+            const int o = off[k - 1] + 16, over = o >= page_size ? 1 : 0;
+            off[k] = o - (over ? page_size : 0);
+            j[k] = j[k - 1] + over;
         }
         ask();
     }
@@ -247,7 +263,7 @@ template <int D> struct StreamShape {
 };
 
 template <typename T, int D, int RP, int RT, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, KvView c, KvTokens t)
+__global__ __launch_bounds__(NW * 64, NW == 4 && D <= 128 && RP <= 8 ? 3 : 2) void attn_stream_kernel(StreamArgs p, KvView c, KvTokens t)
 {
     using Shape = StreamShape<D>;
     constexpr int W = Shape::W, VW = Shape::VW, NJ = Shape::NJ;
@@ -257,21 +273,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
     extern __shared__ float lds[];                         // [NW][ROWS][2], [NW][ROWS][D + 4]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, kg = lane >> 4;
-    int id = blockIdx.x;
-    const int rt = id % p.row_tiles;
-    id /= p.row_tiles;
-    const int h = id % c.heads;
-    id /= c.heads;
-    const int b = id % t.B, split = id / t.B;
-    const int group = p.a.group, row0 = rt * ROWS;
-    const KvLength len = kv_length(t, c, b);
-
-    // what the rows see: lim_lo .. lim_hi tokens
-    const int s_lo = row0 / group, s_hi = min((min(p.rows, row0 + ROWS) - 1) / group, len.count - 1);
-    const bool some = s_lo < len.count;
-    const int lim_lo = some ? min(len.start + s_lo + 1, p.a.max_len) : 0;
-    const int lim_hi = some ? min(len.start + s_hi + 1, p.a.max_len) : 0;
-    const int t0 = split * p.chunk, t1 = min(lim_hi, t0 + p.chunk);
+    const int h = blockIdx.x / p.row_tiles, rt = blockIdx.x - h * p.row_tiles, b = blockIdx.y, split = blockIdx.z;
+    const int group = p.a.group, row0 = rt * ROWS, t0 = split * p.chunk;
 
     float M[RT], l[RT];
     v4f acc[RT][NJ];
@@ -284,280 +287,286 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_stream_kernel(StreamArgs p, K
         for (int j = 0; j < NJ; ++j) acc[x][j] = v4f{0, 0, 0, 0};
     }
 
-    if (t0 + wave * 64 < t1) {
-        // ---- queries
-        v8h q[RT][W];
-        float rowc[RT], q16[RT], q8[RT];
-        int lim[RT];
+    // ---- the first tile's rows are asked for before anything that the lengths decide (every row that the table can lead to is in bounds;
+    // waves without a tile read one for nothing), then the queries: a part's first results wait for two loads in a row, not for four
+    TileRows rows(c, t, b, h, t0 + wave * 64, p.page_jump, p.page_rest);
+    // ---- raw rows
+    uint32_t kraw[4][W], vraw[4][4][VW];
+    int32_t kz[4];
+    v4i vw[4], skw[NB], svw[NB];
+    const int sgrp = col / RP;                          // lane's copy of the rows: blocks sgrp, sgrp + 16 / RP, ..
+    auto own_block = [&](int n) {                       // the row of a lane's n-th block
+        return NB == 4 ? rows.row[n] : NB == 2 ? pick2(rows.row[2 * n & 3], rows.row[(2 * n + 1) & 3], sgrp) : pick4(rows.row[0], rows.row[1], rows.row[2], rows.row[3], sgrp);
+    };
+    auto load_k = [&]() {
 #pragma unroll
-        for (int x = 0; x < RT; ++x) {
-            const int r = min(row0 + x * 16 + (col & (RP - 1)), p.rows - 1), s = r / group;
-            lim[x] = s < len.count ? min(len.start + s + 1, p.a.max_len) : lim_hi;
-            const T *src = (const T *)p.a.q + b * p.a.q_ld_b + s * p.a.q_ld_s + (h * group + (r - s * group)) * p.a.q_ld_h + kg * (D / 4);
-            float f[W][8], top = 0.0f;
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[0] + (uint64_t)rows.row[k] * (D / 2) + (uint32_t)(col * (D / 2) + kg * (D / 8)));
 #pragma unroll
-            for (int j = 0; j < W; ++j) {
-                load_q8<T>(src + 8 * j, p.q_vec, f[j]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[j][i]));
-            }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float power = q_power<T>(top), turn = p.a.scale_log2 < 0.0f ? -power : power;
-            float sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < W; ++j) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    q[x][j][i] = (_Float16)(f[j][i] * turn);
-                    sum += (float)q[x][j][i];
-                }
-            }
-            sum += __shfl_xor(sum, 16);
-            sum += __shfl_xor(sum, 32);
-            q16[x] = -sum * 0x1p-20f;                       // -16 units of every token's zero-point
-            q8[x] = -sum * 0x1p-21f;
-            rowc[x] = fmaxf(fabsf(p.a.scale_log2) * 0x1p20f / power, KV_LEAST);
+            for (int j = 0; j < W; ++j) kraw[k][j] = src[j];
+            kz[k] = (c.words[0] + rows.row[k])[col];
         }
-
-        TileRows rows(c, t, b, h, t0 + wave * 64, p.page_jump, p.page_rest);
-        uint32_t ok = 0;
-
-        // ---- raw rows
-        uint32_t kraw[4][W], vraw[4][4][VW];
-        int32_t kz[4];
-        v4i vw[4], skw[NB], svw[NB];
-        const int sgrp = col / RP;                          // lane's copy of the rows: blocks sgrp, sgrp + 16 / RP, ..
-        auto own_block = [&](int n) {                       // the row of a lane's n-th block
-            return NB == 4 ? rows.row[n] : NB == 2 ? pick2(rows.row[2 * n & 3], rows.row[(2 * n + 1) & 3], sgrp) : pick4(rows.row[0], rows.row[1], rows.row[2], rows.row[3], sgrp);
-        };
-        auto load_k = [&]() {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[0] + (uint64_t)rows.row[k] * (D / 2) + (uint32_t)(col * (D / 2) + kg * (D / 8)));
+        for (int n = 0; n < NB; ++n) {
+            const uint32_t at = own_block(n);
+            skw[n] = *reinterpret_cast<const v4i *>(c.words[0] + at + 4 * kg);
+        }
+    };
+    auto load_v = [&]() {
+        const int word = Shape::HALVES ? col & 7 : D == 96 ? min(col, 11) : VW * col;
 #pragma unroll
-                for (int j = 0; j < W; ++j) kraw[k][j] = src[j];
-                kz[k] = (c.words[0] + rows.row[k])[col];
-            }
+        for (int k = 0; k < 4; ++k) {
+            const uint8_t *src = c.packed[1] + (uint64_t)rows.row[k] * (D / 2) + (uint32_t)(4 * kg * (D / 2) + 4 * word);
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int v = 0; v < VW; ++v) vraw[k][r][v] = reinterpret_cast<const uint32_t *>(src + r * (D / 2))[v];
+            vw[k] = *reinterpret_cast<const v4i *>(c.words[1] + rows.row[k] + 4 * kg);
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            if (NB == 4) {
+                svw[n] = vw[n];
+            } else {
                 const uint32_t at = own_block(n);
-                skw[n] = *reinterpret_cast<const v4i *>(c.words[0] + at + 4 * kg);
+                svw[n] = *reinterpret_cast<const v4i *>(c.words[1] + at + 4 * kg);
             }
-        };
-        auto load_v = [&]() {
-            const int word = Shape::HALVES ? col & 7 : D == 96 ? min(col, 11) : VW * col;
+        }
+    };
+
+    rows.next();
+    load_k();
+    load_v();
+    uint32_t ok = rows.ok;
+
+    // what the rows see: lim_lo .. lim_hi tokens
+    const KvLength len = scalar_length(t, c, b);
+    const int s_lo = row0 / group, s_hi = min((min(p.rows, row0 + ROWS) - 1) / group, len.count - 1);
+    const bool some = s_lo < len.count;
+    const int lim_lo = some ? min(len.start + s_lo + 1, p.a.max_len) : 0;
+    const int lim_hi = some ? min(len.start + s_hi + 1, p.a.max_len) : 0;
+    const int t1 = min(lim_hi, t0 + p.chunk);
+
+    // ---- queries
+    v8h q[RT][W];
+    float rowc[RT], q16[RT], q8[RT];
+    int lim[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const int r = min(row0 + x * 16 + (col & (RP - 1)), p.rows - 1), s = r / group;
+        lim[x] = s < len.count ? min(len.start + s + 1, p.a.max_len) : lim_hi;
+        const T *src = (const T *)p.a.q + b * p.a.q_ld_b + s * p.a.q_ld_s + (h * group + (r - s * group)) * p.a.q_ld_h + kg * (D / 4);
+        float f[W][8], top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            load_q8<T>(src + 8 * j, p.q_vec, f[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[j][i]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float power = q_power<T>(top), turn = p.a.scale_log2 < 0.0f ? -power : power;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                q[x][j][i] = (_Float16)(f[j][i] * turn);
+                sum += (float)q[x][j][i];
+            }
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        q16[x] = -sum * 0x1p-20f;                       // -16 units of every token's zero-point
+        q8[x] = -sum * 0x1p-21f;
+        rowc[x] = fmaxf(fabsf(p.a.scale_log2) * 0x1p20f / power, KV_LEAST);
+    }
+
+    for (int tok = t0 + wave * 64; tok < t1; tok += NW * 64) {
+        const bool more = tok + NW * 64 < t1;
+        // ---- scores: y = sum q (level in units) times the step
+        float y[RT][NB][4];
+        {
+            v4f sc[RT][4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const uint8_t *src = c.packed[1] + (uint64_t)rows.row[k] * (D / 2) + (uint32_t)(4 * kg * (D / 2) + 4 * word);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                for (int x = 0; x < RT; ++x) sc[x][k] = v4f{q8[x], q8[x], q8[x], q8[x]};
+                const uint32_t hi = kv_lut_hi(kz[k]);
 #pragma unroll
-                    for (int v = 0; v < VW; ++v) vraw[k][r][v] = reinterpret_cast<const uint32_t *>(src + r * (D / 2))[v];
-                vw[k] = *reinterpret_cast<const v4i *>(c.words[1] + rows.row[k] + 4 * kg);
-            }
+                for (int j = 0; j < W; ++j) {
+                    const uint32_t lo4 = kv_bytes(kraw[k][j], hi), hi4 = kv_bytes(kraw[k][j] >> 4, hi);
+                    const v4u n = {__builtin_amdgcn_perm(0u, lo4, 0x0c010c00u), __builtin_amdgcn_perm(0u, lo4, 0x0c030c02u),
+                                   __builtin_amdgcn_perm(0u, hi4, 0x0c010c00u), __builtin_amdgcn_perm(0u, hi4, 0x0c030c02u)};
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                if (NB == 4) {
-                    svw[n] = vw[n];
-                } else {
-                    const uint32_t at = own_block(n);
-                    svw[n] = *reinterpret_cast<const v4i *>(c.words[1] + at + 4 * kg);
+                    for (int x = 0; x < RT; ++x)
+                        sc[x][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, n), q[x][j], sc[x][k], 0, 0, 0);
                 }
             }
-        };
-
-        rows.next();
-        load_k();
-        load_v();
-        ok = rows.ok;
-
-        for (int tok = t0 + wave * 64; tok < t1; tok += NW * 64) {
-            const bool more = tok + NW * 64 < t1;
-            // ---- scores: y = sum q (level in units) times the step
-            float y[RT][NB][4];
-            {
-                v4f sc[RT][4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-#pragma unroll
-                    for (int x = 0; x < RT; ++x) sc[x][k] = v4f{q8[x], q8[x], q8[x], q8[x]};
-                    const uint32_t hi = kv_lut_hi(kz[k]);
-#pragma unroll
-                    for (int j = 0; j < W; ++j) {
-                        const uint32_t lo4 = kv_bytes(kraw[k][j], hi), hi4 = kv_bytes(kraw[k][j] >> 4, hi);
-                        const v4u n = {__builtin_amdgcn_perm(0u, lo4, 0x0c010c00u), __builtin_amdgcn_perm(0u, lo4, 0x0c030c02u),
-                                       __builtin_amdgcn_perm(0u, hi4, 0x0c010c00u), __builtin_amdgcn_perm(0u, hi4, 0x0c030c02u)};
-#pragma unroll
-                        for (int x = 0; x < RT; ++x)
-                            sc[x][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, n), q[x][j], sc[x][k], 0, 0, 0);
-                    }
-                }
-#pragma unroll
-                for (int x = 0; x < RT; ++x)
-#pragma unroll
-                    for (int n = 0; n < NB; ++n)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            float a = sc[x][n * (4 / NB)][r];
-#pragma unroll
-                            for (int k = 1; k < 4 / NB; ++k) a = sgrp == k ? sc[x][n * (4 / NB) + k][r] : a;
-                            const int32_t w = skw[n][r];
-                            y[x][n][r] = __builtin_fmaf((float)(w & 15), q16[x], a) * __int_as_float(w & -16);
-                        }
-            }
-            const bool whole = ok == 15u && tok + 64 <= lim_lo;
-            if (more) {
-                rows.next();
-                load_k();
-            }
-            // ---- softmax
-            if (!whole) {
-                int end[RT];                                // (through the statement below, so that this stays a branch)
-#pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    end[x] = lim[x];
-                    asm volatile("" : "+v"(end[x]));
-                }
-                uint32_t seen[NB][4];                       // (a token that no row sees may hold anything: its step is not used)
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int k = n * (4 / NB) + (NB == 4 ? 0 : sgrp);
-                        bool any = false;
-#pragma unroll
-                        for (int x = 0; x < RT; ++x) {
-                            const bool in = tok + 16 * k + 4 * kg + r < end[x] && (ok >> k & 1u);
-                            y[x][n][r] = in ? y[x][n][r] : KV_MASKED;
-                            any = any || in;
-                        }
-                        seen[n][r] = any ? (uint32_t)svw[n][r] : 0u;
-                    }
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) svw[n][r] = (int)seen[n][r];
-            }
-            float top[RT];
-            uint32_t top_step = 0;
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) top_step = max(top_step, (uint32_t)svw[n][r] & 0x7fffffffu);
-            bool move = false;
-#pragma unroll
-            for (int x = 0; x < RT; ++x) {
-                top[x] = y[x][0][0];
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) top[x] = fmaxf(top[x], y[x][n][r]);
-                top[x] *= rowc[x];
-                move = move || top[x] > M[x] + KV_SLACK;
-            }
-            if (__builtin_amdgcn_ballot_w64((int)(top_step >> 23) - 127 > E)) {   // rare: a larger step
-                const int E_new = max(E, (int)wave_max_u32(top_step >> 23) - 127);
-                const float shift = __builtin_ldexpf(1.0f, E - E_new);
-                E = E_new;
-#pragma unroll
-                for (int x = 0; x < RT; ++x)
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j) acc[x][j] *= shift;
-            }
-            if (__builtin_amdgcn_ballot_w64(move)) {        // rare: larger scores
-#pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    float m = fmaxf(top[x], M[x] - KV_AHEAD);
-                    m = max_xor32(max_xor16(m));
-                    if (RP <= 8) m = fmaxf(m, dpp_f32<DPP_ROW_ROR8>(m));
-                    if (RP <= 4) m = fmaxf(m, dpp_f32<DPP_ROW_ROR4>(m));
-                    m = m > M[x] - KV_AHEAD ? m + KV_AHEAD : M[x];
-                    const float keep = __builtin_amdgcn_exp2f(M[x] - m);
-                    M[x] = m;
-                    l[x] *= keep;
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j) acc[x][j] *= keep;
-                }
-            }
-            const float unit = __builtin_ldexpf(1.0f, 12 - E);
-            uint32_t w2[RT][NB][2];                         // weights, two to a word
 #pragma unroll
             for (int x = 0; x < RT; ++x)
 #pragma unroll
-                for (int n = 0; n < NB; ++n) {
-                    float wv[4];
+                for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[x][n][r], rowc[x], -M[x]));
-                        wv[r] = pr * (__int_as_float(svw[n][r] & -16) * unit);
-                        l[x] += pr;
-                    }
+                        float a = sc[x][n * (4 / NB)][r];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const v2h pair = __builtin_convertvector((v2f{wv[2 * i], wv[2 * i + 1]}), v2h);
-                        w2[x][n][i] = __builtin_bit_cast(uint32_t, pair);
+                        for (int k = 1; k < 4 / NB; ++k) a = sgrp == k ? sc[x][n * (4 / NB) + k][r] : a;
+                        const int32_t w = skw[n][r];
+                        y[x][n][r] = __builtin_fmaf((float)(w & 15), q16[x], a) * __int_as_float(w & -16);
                     }
+        }
+        const bool whole = ok == 15u && tok + 64 <= lim_lo;
+        if (more) {
+            rows.next();
+            load_k();
+        }
+        // ---- softmax
+        if (!whole) {
+            int end[RT];                                // (through the statement below, so that this stays a branch)
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                end[x] = lim[x];
+                asm volatile("" : "+v"(end[x]));
+            }
+            uint32_t seen[NB][4];                       // (a token that no row sees may hold anything: its step is not used)
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int k = n * (4 / NB) + (NB == 4 ? 0 : sgrp);
+                    bool any = false;
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) {
+                        const bool in = tok + 16 * k + 4 * kg + r < end[x] && (ok >> k & 1u);
+                        y[x][n][r] = in ? y[x][n][r] : KV_MASKED;
+                        any = any || in;
+                    }
+                    seen[n][r] = any ? (uint32_t)svw[n][r] : 0u;
                 }
-            // ---- the product with the Values, 32 tokens at a time
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                v8h wop[RT];
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    v4u o;
-                    if (NB == 4) {
-                        o = v4u{w2[x][2 * half][0], w2[x][2 * half][1], w2[x][2 * half + 1][0], w2[x][2 * half + 1][1]};
-                    } else if (NB == 2) {                   // block 2 half + 1 lies eight lanes on
-                        o = v4u{w2[x][half][0], w2[x][half][1], (uint32_t)dpp_i32<DPP_ROW_ROR8>((int)w2[x][half][0]),
-                                (uint32_t)dpp_i32<DPP_ROW_ROR8>((int)w2[x][half][1])};
-                    } else {                                // blocks 1, 2, 3 four, eight, twelve lanes on
-                        const int a = (int)w2[x][0][0], b2 = (int)w2[x][0][1];
-                        if (half == 0)
-                            o = v4u{(uint32_t)a, (uint32_t)b2, (uint32_t)dpp_i32<0x12C>(a), (uint32_t)dpp_i32<0x12C>(b2)};
-                        else
-                            o = v4u{(uint32_t)dpp_i32<DPP_ROW_ROR8>(a), (uint32_t)dpp_i32<DPP_ROW_ROR8>(b2),
-                                    (uint32_t)dpp_i32<DPP_ROW_ROR4>(a), (uint32_t)dpp_i32<DPP_ROW_ROR4>(b2)};
-                    }
-                    wop[x] = __builtin_bit_cast(v8h, o);
+                for (int r = 0; r < 4; ++r) svw[n][r] = (int)seen[n][r];
+        }
+        float top[RT];
+        uint32_t top_step = 0;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top_step = max(top_step, (uint32_t)svw[n][r] & 0x7fffffffu);
+        bool move = false;
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            top[x] = y[x][0][0];
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top[x] = fmaxf(top[x], y[x][n][r]);
+            top[x] *= rowc[x];
+            move = move || top[x] > M[x] + KV_SLACK;
+        }
+        if (__builtin_amdgcn_ballot_w64((int)(top_step >> 23) - 127 > E)) {   // rare: a larger step
+            const int E_new = max(E, (int)wave_max_u32(top_step >> 23) - 127);
+            const float shift = __builtin_ldexpf(1.0f, E - E_new);
+            E = E_new;
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[x][j] *= shift;
+        }
+        if (__builtin_amdgcn_ballot_w64(move)) {        // rare: larger scores
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                float m = fmaxf(top[x], M[x] - KV_AHEAD);
+                m = max_xor32(max_xor16(m));
+                if (RP <= 8) m = fmaxf(m, dpp_f32<DPP_ROW_ROR8>(m));
+                if (RP <= 4) m = fmaxf(m, dpp_f32<DPP_ROW_ROR4>(m));
+                m = m > M[x] - KV_AHEAD ? m + KV_AHEAD : M[x];
+                const float keep = __builtin_amdgcn_exp2f(M[x] - m);
+                M[x] = m;
+                l[x] *= keep;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[x][j] *= keep;
+            }
+        }
+        const float unit = __builtin_ldexpf(1.0f, 12 - E);
+        uint32_t w2[RT][NB][2];                         // weights, two to a word
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                float wv[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(y[x][n][r], rowc[x], -M[x]));
+                    wv[r] = pr * (__int_as_float(svw[n][r] & -16) * unit);
+                    l[x] += pr;
                 }
 #pragma unroll
-                for (int v = 0; v < VW; ++v) {
-                    uint32_t lo4[8], hi4[8], lut[8];
-                    v2h zero[4];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int k = 2 * half + i / 4, r = i % 4;
-                        const uint32_t hi = lut[i] = kv_lut_hi(vw[k][r]);
-                        if (Shape::HALVES) {
-                            lo4[i] = kv_bytes(vraw[k][r][v] >> (col >= 8 ? 4 : 0), hi);
-                        } else {
-                            lo4[i] = kv_bytes(vraw[k][r][v], hi);
-                            hi4[i] = kv_bytes(vraw[k][r][v] >> 4, hi);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)             // 16 z + 8 of two tokens
-                        zero[i] = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(lut[2 * i + 1], lut[2 * i], 0x0c070c03u) | 0x00080008u);
-#pragma unroll
-                    for (int j = 0; j < (Shape::HALVES ? 4 : 8); ++j) {
-                        const uint32_t sel = 0x0c040c00u + (uint32_t)(j & 3) * 0x00010001u;
-                        v4u n;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t two = j < 4 ? __builtin_amdgcn_perm(lo4[2 * i + 1], lo4[2 * i], sel) : __builtin_amdgcn_perm(hi4[2 * i + 1], hi4[2 * i], sel);
-                            n[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, two) - zero[i]);
-                        }
-#pragma unroll
-                        for (int x = 0; x < RT; ++x)
-                            acc[x][v * 8 + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, n), wop[x], acc[x][v * 8 + j], 0, 0, 0);
-                    }
+                for (int i = 0; i < 2; ++i) {
+                    const v2h pair = __builtin_convertvector((v2f{wv[2 * i], wv[2 * i + 1]}), v2h);
+                    w2[x][n][i] = __builtin_bit_cast(uint32_t, pair);
                 }
             }
-            if (more) {
-                load_v();
-                ok = rows.ok;
+        // ---- the product with the Values, 32 tokens at a time
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            v8h wop[RT];
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                v4u o;
+                if (NB == 4) {
+                    o = v4u{w2[x][2 * half][0], w2[x][2 * half][1], w2[x][2 * half + 1][0], w2[x][2 * half + 1][1]};
+                } else if (NB == 2) {                   // block 2 half + 1 lies eight lanes on
+                    o = v4u{w2[x][half][0], w2[x][half][1], (uint32_t)dpp_i32<DPP_ROW_ROR8>((int)w2[x][half][0]),
+                            (uint32_t)dpp_i32<DPP_ROW_ROR8>((int)w2[x][half][1])};
+                } else {                                // blocks 1, 2, 3 four, eight, twelve lanes on
+                    const int a = (int)w2[x][0][0], b2 = (int)w2[x][0][1];
+                    if (half == 0)
+                        o = v4u{(uint32_t)a, (uint32_t)b2, (uint32_t)dpp_i32<0x12C>(a), (uint32_t)dpp_i32<0x12C>(b2)};
+                    else
+                        o = v4u{(uint32_t)dpp_i32<DPP_ROW_ROR8>(a), (uint32_t)dpp_i32<DPP_ROW_ROR8>(b2),
+                                (uint32_t)dpp_i32<DPP_ROW_ROR4>(a), (uint32_t)dpp_i32<DPP_ROW_ROR4>(b2)};
+                }
+                wop[x] = __builtin_bit_cast(v8h, o);
             }
+#pragma unroll
+            for (int v = 0; v < VW; ++v) {
+                uint32_t lo4[8], hi4[8], lut[8];
+                v2h zero[4];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int k = 2 * half + i / 4, r = i % 4;
+                    const uint32_t hi = lut[i] = kv_lut_hi(vw[k][r]);
+                    if (Shape::HALVES) {
+                        lo4[i] = kv_bytes(vraw[k][r][v] >> (col >= 8 ? 4 : 0), hi);
+                    } else {
+                        lo4[i] = kv_bytes(vraw[k][r][v], hi);
+                        hi4[i] = kv_bytes(vraw[k][r][v] >> 4, hi);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)             // 16 z + 8 of two tokens
+                    zero[i] = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(lut[2 * i + 1], lut[2 * i], 0x0c070c03u) | 0x00080008u);
+#pragma unroll
+                for (int j = 0; j < (Shape::HALVES ? 4 : 8); ++j) {
+                    const uint32_t sel = 0x0c040c00u + (uint32_t)(j & 3) * 0x00010001u;
+                    v4u n;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t two = j < 4 ? __builtin_amdgcn_perm(lo4[2 * i + 1], lo4[2 * i], sel) : __builtin_amdgcn_perm(hi4[2 * i + 1], hi4[2 * i], sel);
+                        n[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, two) - zero[i]);
+                    }
+#pragma unroll
+                    for (int x = 0; x < RT; ++x)
+                        acc[x][v * 8 + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, n), wop[x], acc[x][v * 8 + j], 0, 0, 0);
+                }
+            }
+        }
+        if (more) {
+            load_v();
+            ok = rows.ok;
         }
     }
 
@@ -674,14 +683,11 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
     // longest tiles first, and the row tiles of a (sequence, head) in runs of TILE_RUN: workgroups go to an XCD's four shader engines in
     // turn whether these are busy or not, so a period of 2 or 4 in what they have to do would leave engines idle (two sequences of
     // 3000 and 743 tokens, the short one's empty workgroups every second place: 226 us; in runs 160)
-    const int h = id % c.heads;
-    id /= c.heads;
-    const int run = min(TILE_RUN, p.row_tiles), in_run = id % run;
-    id /= run;
-    const int b = id % t.B, rt = p.row_tiles - 1 - (id / t.B * run + in_run);
+    const int in_run = id / c.heads, h = id - in_run * c.heads, b = blockIdx.y;
+    const int rt = p.row_tiles - 1 - ((int)blockIdx.z * min(TILE_RUN, p.row_tiles) + in_run);
     if (rt < 0) return;
     const int group = p.a.group, row0 = rt * NW * 32, wrow0 = row0 + wave * 32;
-    const KvLength len = kv_length(t, c, b);
+    const KvLength len = scalar_length(t, c, b);
     auto limit = [&](int r) { return min(len.start + r / group + 1, p.a.max_len); };    // tokens that a row sees, if it is there
     const int there = min(p.rows, len.count * group);                                   // rows that are there
     const int lim_wg = row0 < there ? limit(min(row0 + NW * 32, there) - 1) : 0;
@@ -987,21 +993,21 @@ __global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_kernel(StreamArgs p, int heads, int S, int D, int ways, int64_t all_rows)
 {
-    __shared__ float red[5][256];
+    __shared__ float red[6][256];
     const int quad = D / 4, groups = 256 / quad, per = groups / ways;
     const int g = threadIdx.x / quad, ch = (threadIdx.x - g * quad) * 4, way = g / per;
     const int64_t at = (int64_t)blockIdx.x * per + (g - way * per);
     const bool mine = way < ways && at < all_rows;
     const float *ml = p.part_ml + at * p.splits * 2, *po = p.part_o + at * p.splits * D + ch;
-    // every lane looks over all maxima of its row (they are few, and in cache after the first), so the groups agree on it
     float m = KV_NONE, sum = 0.0f;
     v4f o = {0, 0, 0, 0};
     if (mine) {
-        for (int s = 0; s < p.splits; ++s) {
+#pragma unroll 8
+        for (int s = way; s < p.splits; s += ways) {
             const v2f x = *reinterpret_cast<const v2f *>(ml + 2 * s);
             m = x[1] > 0.0f ? fmaxf(m, x[0]) : m;
         }
-#pragma unroll 4
+#pragma unroll 8
         for (int s = way; s < p.splits; s += ways) {
             const v2f x = *reinterpret_cast<const v2f *>(ml + 2 * s);
             if (x[1] > 0.0f) {                              // (a part without tokens was not written)
@@ -1015,13 +1021,20 @@ __global__ __launch_bounds__(256) void attn_join_kernel(StreamArgs p, int heads,
 #pragma unroll
         for (int i = 0; i < 4; ++i) red[i][threadIdx.x] = o[i];
         red[4][threadIdx.x] = sum;
+        red[5][threadIdx.x] = m;
         __syncthreads();
         if (mine && way == 0) {
+            float top = m;
+            for (int w = 1; w < ways; ++w) top = fmaxf(top, red[5][threadIdx.x + w * per * quad]);
+            const float own = __builtin_amdgcn_exp2f(m - top);
+            o *= own;
+            sum *= own;
             for (int w = 1; w < ways; ++w) {
                 const int from = threadIdx.x + w * per * quad;
+                const float f = __builtin_amdgcn_exp2f(red[5][from] - top);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] += red[i][from];
-                sum += red[4][from];
+                for (int i = 0; i < 4; ++i) o[i] += red[i][from] * f;
+                sum += red[4][from] * f;
             }
         }
     }
@@ -1089,7 +1102,8 @@ static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, in
     const bool pages = c.page_ld < 1LL << 32 && c.head_ld < 1LL << 32 && c.page_size % 16 == 0 && c.page_ld % 16 == 0 && c.head_ld % 16 == 0 && c.pages > 0 && t.table_cols > 0 &&
                        (c.pages - 1) * c.page_ld + (c.heads - 1) * c.head_ld + c.page_size < 1LL << 32;
     if (dtype == W4A8_F32 || !pages || (c.D != 64 && c.D != 96 && c.D != 128 && c.D != 256)) return n;
-    if (rows > 0x7fffffffLL / 2) return n;
+    // (what the grids and the positions' 32 bits hold: everything else goes row by row)
+    if (rows > 1 << 23 || t.B > 65535 || (int64_t)t.table_cols * c.page_size > 1 << 30) return n;
     const int64_t tokens = std::max<int64_t>(1, std::min<int64_t>(max_len, (int64_t)t.table_cols * c.page_size));
     const int64_t pairs = (int64_t)t.B * c.heads;
     auto cut = [&](int64_t want, int64_t most) {
@@ -1110,10 +1124,15 @@ static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, in
     }
     n.stream = rows <= 16 || c.D == 256 ? 1 : 2;
     n.rp = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
-    n.waves = 8;
+    // Many sequences and heads: workgroups of four waves, three to a CU (as the registers allow), keep more loads in flight than one of
+    // eight (32 x 4096 tokens, 40 heads: 164 us for 185); few: eight waves per part, i.e. half as many parts to join (131073
+    // tokens, 8 heads: 49 us for 58; 600 tokens, 32 heads: 9.0 for 11.7).
+    n.waves = pairs >= 512 ? 4 : 8;
     n.row_tiles = (int)((rows + 16 * n.stream - 1) / (16 * n.stream));
     const int64_t tile = n.waves * 64;
-    cut(1024 / pairs, (tokens + 2 * tile - 1) / (2 * tile));
+    // One workgroup to a CU at a time (registers), so as many parts as there are CUs: each is as long as it can be, and the queries, the
+    // waves' join and the parts' join are paid for once.  131073 tokens, 8 heads (32 parts): 50 us, 64 parts 62, 128 parts 79.
+    cut(256 / pairs, (tokens + 2 * tile - 1) / (2 * tile));
     return n;
 }
 
@@ -1123,19 +1142,18 @@ size_t attention_kv_workspace(int dtype, const KvView &c, const KvTokens &t, int
     return n.part_bytes + n.ml_bytes;
 }
 
-template <typename T, int D, int RP, int RT>
+template <typename T, int D, int RP, int RT, int NW>
 static int launch_stream(const StreamArgs &p, const KvView &c, const KvTokens &t, hipStream_t st)
 {
-    constexpr int NW = 8, ROWS = RP * RT;
+    constexpr int ROWS = RP * RT;
     constexpr int bytes = NW * ROWS * (2 + D + 4) * 4;
     static std::atomic<uint64_t> done{0};
     if (bytes > 65536) {
         const int rc = opt_in_dynamic_lds((const void *)attn_stream_kernel<T, D, RP, RT, NW>, bytes, done);
         if (rc != W4A8_OK) return rc;
     }
-    const int64_t blocks = (int64_t)t.B * c.heads * p.row_tiles * p.splits;
-    if (blocks > 0x7fffffffLL) return W4A8_ERR_SHAPE;
-    hipLaunchKernelGGL((attn_stream_kernel<T, D, RP, RT, NW>), dim3((unsigned)blocks), dim3(NW * 64), bytes, st, p, c, t);
+    const dim3 grid((unsigned)(c.heads * p.row_tiles), (unsigned)t.B, (unsigned)p.splits);
+    hipLaunchKernelGGL((attn_stream_kernel<T, D, RP, RT, NW>), grid, dim3(NW * 64), bytes, st, p, c, t);
     return launch_join<T>(p, c, t, st);
 }
 
@@ -1148,10 +1166,9 @@ static int launch_tile(const StreamArgs &p, const KvView &c, const KvTokens &t, 
         const int rc = opt_in_dynamic_lds((const void *)attn_tile_kernel<T, D, NW>, bytes, done);
         if (rc != W4A8_OK) return rc;
     }
-    const int64_t run = std::min(TILE_RUN, p.row_tiles);
-    const int64_t blocks = (int64_t)t.B * c.heads * ((p.row_tiles + run - 1) / run * run) * p.splits;
-    if (blocks > 0x7fffffffLL) return W4A8_ERR_SHAPE;
-    hipLaunchKernelGGL((attn_tile_kernel<T, D, NW>), dim3((unsigned)blocks), dim3(NW * 64), bytes, st, p, c, t);
+    const int run = std::min(TILE_RUN, p.row_tiles);
+    const dim3 grid((unsigned)(p.splits * c.heads * run), (unsigned)t.B, (unsigned)((p.row_tiles + run - 1) / run));
+    hipLaunchKernelGGL((attn_tile_kernel<T, D, NW>), grid, dim3(NW * 64), bytes, st, p, c, t);
     return launch_join<T>(p, c, t, st);
 }
 
@@ -1164,12 +1181,12 @@ static int launch_stream_d(const AttnPlan &n, const StreamArgs &p, const KvView 
     }
     if (n.tile == 4) return launch_tile<T, D, 4>(p, c, t, st);
     if (n.stream == 2) {
-        if constexpr (D <= 128) return launch_stream<T, D, 16, 2>(p, c, t, st);
+        if constexpr (D <= 128) return n.waves == 4 ? launch_stream<T, D, 16, 2, 4>(p, c, t, st) : launch_stream<T, D, 16, 2, 8>(p, c, t, st);
         return W4A8_ERR_SHAPE;
     }
-    if (n.rp == 4) return launch_stream<T, D, 4, 1>(p, c, t, st);
-    if (n.rp == 8) return launch_stream<T, D, 8, 1>(p, c, t, st);
-    return launch_stream<T, D, 16, 1>(p, c, t, st);
+    if (n.rp == 4) return n.waves == 4 ? launch_stream<T, D, 4, 1, 4>(p, c, t, st) : launch_stream<T, D, 4, 1, 8>(p, c, t, st);
+    if (n.rp == 8) return n.waves == 4 ? launch_stream<T, D, 8, 1, 4>(p, c, t, st) : launch_stream<T, D, 8, 1, 8>(p, c, t, st);
+    return n.waves == 4 ? launch_stream<T, D, 16, 1, 4>(p, c, t, st) : launch_stream<T, D, 16, 1, 8>(p, c, t, st);
 }
 
 template <typename T>
