@@ -11,6 +11,8 @@
 //     bits and step 20, so u is either a half-integer or at least 2^-21 from one, and u < 16 is rounded by at most that: rne(u)
 //     is that of the exact quotient.  (binary32 inputs: by this u.)
 //   - the step's half-up at bit 20 looks at the sign of the division's remainder, what hi - lo lost included.
+#include <algorithm>
+
 #include "kv_dint4.hpp"
 #include "row_quant.hpp"
 
@@ -24,9 +26,12 @@ struct KvRows {            // [B][S][heads][D], D contiguous
     int64_t ld_b[2], ld_s[2], ld_h[2];
 };
 
-// How a wave's 64 / L groups of L lanes are spent: on `tokens` consecutive tokens of 64 / L / tokens consecutive heads
+// How a wave's 64 / L groups of L lanes are spent: on 2^tokens_log consecutive tokens of 64 / L / 2^tokens_log consecutive heads (many
+// tokens: a group's bytes in the cache follow one another); a workgroup's four waves take consecutive heads.  Page numbers come
+// from positions by a multiplication: position / page_size = high word of position * magic, shifted.
 struct KvTiles {
-    int tokens_log, s_tiles, h_tiles;
+    int tokens_log, s_tiles, shift;
+    uint32_t magic;        // 0: pages of one token
 };
 
 struct RowScale {
@@ -38,16 +43,17 @@ __device__ __forceinline__ RowScale row_scale(float lo_neg, float hi)
     RowScale r;
     const float d = hi + lo_neg, back = d - hi;
     const float lost = (hi - (d - back)) + (lo_neg - back);          // hi + lo_neg = d + lost exactly
-    const float q = d / 13.0f;
-    // half up at the last four bits of (d + lost) / 13, whose nearest binary32 number is within two units of q: the sign of
-    // 13 (q - border) + (d - 13 q) + lost; the first two terms are exact, and so is their sum
+    // half up at the last four bits of (d + lost) / 13, which is within two units of q: the sign of 13 (q - border) + (d - 13 q) +
+    // lost, where the first two terms are exact, and so is their sum
+    const float q = d * (1.0f / 13.0f);
     const uint32_t base = __float_as_uint(q) & ~15u;
     const float rem = __builtin_fmaf(q - __uint_as_float(base + 8u), 13.0f, __builtin_fmaf(-q, 13.0f, d)) + lost;
     const float step = __uint_as_float(base + (rem >= 0.0f ? 16u : 0u));
     const bool live = step >= KV_F32_MIN;
+    const float inv = __builtin_amdgcn_rcpf(step);         // (within a unit: inv_lo has what it lacks)
     r.step = live ? step : 0.0f;
-    r.inv = live ? 1.0f / step : 0.0f;
-    r.inv_lo = live ? __builtin_fmaf(-r.inv, step, 1.0f) * r.inv : 0.0f;
+    r.inv = live ? inv : 0.0f;
+    r.inv_lo = live ? __builtin_fmaf(-inv, step, 1.0f) * inv : 0.0f;
     const float z = __builtin_fmaf(lo_neg, r.inv, lo_neg * r.inv_lo);
     r.zero = fminf(__builtin_rintf(z), 13.0f);
     return r;
@@ -70,62 +76,54 @@ __device__ __forceinline__ uint32_t encode8(const float (&x)[8], const RowScale 
     return recode8(pack4_low_bytes(c[0], c[1], c[2], c[3]), pack4_low_bytes(c[4], c[5], c[6], c[7]), 0x01010101u);
 }
 
-// A row's place: which (b, s, head) a group of lanes has, and whether there is such a row
-struct KvPlace {
-    int b, s, head;
-    bool in;
-};
-template <int L>
-__device__ __forceinline__ KvPlace kv_place(const KvTokens &t, const KvView &c, const KvTiles &n)
+__device__ __forceinline__ int64_t kv_place(const KvTokens &t, const KvView &c, const KvTiles &n, int b, int head, int token)
 {
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int g = (threadIdx.x & 63) / L, tokens = 1 << n.tokens_log, heads = 64 / L >> n.tokens_log;
-    const int64_t rest = wave / n.h_tiles;
-    KvPlace p;
-    p.head = (int)(wave - rest * n.h_tiles) * heads + (g >> n.tokens_log);
-    p.b = (int)(rest / n.s_tiles);
-    p.s = (int)(rest - (int64_t)p.b * n.s_tiles) * tokens + (g & (tokens - 1));
-    p.in = p.b < t.B && p.s < t.S && p.head < c.heads;
-    return p;
+    const int j = n.magic ? (int)(__umulhi((uint32_t)token, n.magic) >> n.shift) : token;
+    const int64_t page = t.table[b * t.table_ld + j];
+    return page < 0 || page >= c.pages ? -1 : page * c.page_ld + head * c.head_ld + (token - j * c.page_size);
 }
 
 // L lanes (8 channels each) per row, Keys and Values of it
 template <typename T, int L, bool VEC>
 __global__ __launch_bounds__(256) void kv_write_kernel(KvRows in, KvView c, KvTokens t, KvTiles n)
 {
-    const KvPlace at = kv_place<L>(t, c, n);
-    const int lane = threadIdx.x & (L - 1), words = c.D / 8;
-    bool there = at.in;
-    int64_t row = -1;
-    if (there) {
-        const KvLength len = kv_length(t, c, at.b);
-        there = at.s < len.count;
-        if (there) row = kv_row(t, c, at.b, at.head, len.start + at.s);
-        there = row >= 0;
-    }
-    const bool mine = there && lane < words;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & (L - 1), g = (threadIdx.x & 63) / L, words = c.D / 8;
+    const int heads = 64 / L >> n.tokens_log, head = (blockIdx.x * 4 + wave) * heads + (g >> n.tokens_log);
+    for (int b = blockIdx.z; b < t.B; b += gridDim.z) {
+        const KvLength len = kv_length(t, c, b);
+        for (int tile = blockIdx.y; tile < n.s_tiles; tile += gridDim.y) {
+            const int s = (tile << n.tokens_log) + (g & ((1 << n.tokens_log) - 1));
+            const bool there = s < len.count && head < c.heads;
+            float x[2][8];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (mine) {
-            const T *p = (const T *)in.x[kv] + at.b * in.ld_b[kv] + at.s * in.ld_s[kv] + at.head * in.ld_h[kv] + lane * 8;
-            if (VEC) {
-                load8<T>(p, x);
-            } else {
+            for (int kv = 0; kv < 2; ++kv) {                // (both rows' loads go out before their place is looked up)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = to_f32(p[j]);
+                for (int j = 0; j < 8; ++j) x[kv][j] = 0.0f;
+                if (there && lane < words) {
+                    const T *p = (const T *)in.x[kv] + b * in.ld_b[kv] + s * in.ld_s[kv] + head * in.ld_h[kv] + lane * 8;
+                    if (VEC) {
+                        widen8(load_raw8<T>(p), x[kv]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[kv][j] = to_f32(p[j]);
+                    }
+                }
             }
-        }
-        float lo = 0.0f, hi = 0.0f;
+            const int64_t row = there ? kv_place(t, c, n, b, head, len.start + s) : -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            lo = fmaxf(lo, -x[j]);
-            hi = fmaxf(hi, x[j]);
-        }
-        const RowScale r = row_scale(group_max<L>(lo), group_max<L>(hi));
-        if (mine) {
-            reinterpret_cast<uint32_t *>(c.packed[kv])[row * words + lane] = encode8(x, r);
-            if (lane == 0) c.words[kv][row] = __float_as_int(r.step) | (int)r.zero;
+            for (int kv = 0; kv < 2; ++kv) {
+                float lo = 0.0f, hi = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    lo = fmaxf(lo, -x[kv][j]);
+                    hi = fmaxf(hi, x[kv][j]);
+                }
+                const RowScale r = row_scale(group_max<L>(lo), group_max<L>(hi));
+                if (row >= 0 && lane < words) {
+                    reinterpret_cast<uint32_t *>(c.packed[kv])[row * words + lane] = encode8(x[kv], r);
+                    if (lane == 0) c.words[kv][row] = __float_as_int(r.step) | (int)r.zero;
+                }
+            }
         }
     }
 }
@@ -158,45 +156,52 @@ __device__ __forceinline__ void store8<bf16_t>(bf16_t *p, const float (&v)[8])
 template <typename T, int L>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvRows out, KvView c, KvTokens t, KvTiles n)
 {
-    const KvPlace at = kv_place<L>(t, c, n);
-    const int lane = threadIdx.x & (L - 1), words = c.D / 8;
-    if (!at.in || lane >= words) return;
-    const KvLength len = kv_length(t, c, at.b);
-    const int64_t row = at.s < len.count ? kv_row(t, c, at.b, at.head, len.start + at.s) : -1;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & (L - 1), g = (threadIdx.x & 63) / L, words = c.D / 8;
+    const int heads = 64 / L >> n.tokens_log, head = (blockIdx.x * 4 + wave) * heads + (g >> n.tokens_log);
+    if (lane >= words || head >= c.heads) return;
+    for (int b = blockIdx.z; b < t.B; b += gridDim.z) {
+        const KvLength len = kv_length(t, c, b);
+        for (int tile = blockIdx.y; tile < n.s_tiles; tile += gridDim.y) {
+            const int s = (tile << n.tokens_log) + (g & ((1 << n.tokens_log) - 1));
+            if (s >= t.S) continue;
+            const int64_t row = s < len.count ? kv_place(t, c, n, b, head, len.start + s) : -1;
+            uint32_t p[2] = {0, 0};
+            int32_t word[2] = {0, 0};
+            if (row >= 0) {
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (row >= 0) {
-            const int32_t word = c.words[kv][row];
-            kv_decode8(reinterpret_cast<const uint32_t *>(c.packed[kv])[row * words + lane], make_decode_lut(word & 15), v);
-            const float unit = 0.125f * kv_step(word);   // (20 bits and above the subnormals by 2^3 at least where it matters)
+                for (int kv = 0; kv < 2; ++kv) {
+                    p[kv] = reinterpret_cast<const uint32_t *>(c.packed[kv])[row * words + lane];
+                    word[kv] = c.words[kv][row];
+                }
+            }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= unit;
+            for (int kv = 0; kv < 2; ++kv) {                // (no row: code 0 under a step and zero-point of 0)
+                float v[8];
+                kv_decode8(p[kv], make_decode_lut(word[kv] & 15), v);
+                const float unit = 0.125f * kv_step(word[kv]);   // (20 bits: exact)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= unit;
+                store8<T>((T *)out.x[kv] + b * out.ld_b[kv] + s * out.ld_s[kv] + head * out.ld_h[kv] + lane * 8, v);
+            }
         }
-        store8<T>((T *)out.x[kv] + at.b * out.ld_b[kv] + at.s * out.ld_s[kv] + at.head * out.ld_h[kv] + lane * 8, v);
     }
-}
-
-static KvTiles kv_tiles(const KvTokens &t, const KvView &c, int L, int64_t &blocks)
-{
-    KvTiles n;
-    const int groups = 64 / L;
-    n.tokens_log = 0;
-    while (1 << n.tokens_log < groups && 1 << n.tokens_log < t.S) ++n.tokens_log;
-    const int tokens = 1 << n.tokens_log, heads = groups / tokens;
-    n.s_tiles = (t.S + tokens - 1) / tokens;
-    n.h_tiles = (c.heads + heads - 1) / heads;
-    blocks = ((int64_t)t.B * n.s_tiles * n.h_tiles + 3) / 4;
-    return n;
 }
 
 template <typename T, int L>
 static int launch_kv(bool write, const KvRows &rows, const KvView &c, const KvTokens &t, bool vec, hipStream_t st)
 {
-    int64_t blocks;
-    const KvTiles n = kv_tiles(t, c, L, blocks);
-    if (blocks > 0x7fffffffLL) return W4A8_ERR_SHAPE;
-    const dim3 grid((unsigned)blocks), block(256);
+    KvTiles n = {0, 0, 0, 0};
+    const int groups = 64 / L;
+    while (1 << n.tokens_log < groups && 1 << n.tokens_log < t.S) ++n.tokens_log;
+    const int tokens = 1 << n.tokens_log, heads = 4 * (groups / tokens);
+    n.s_tiles = (t.S + tokens - 1) / tokens;
+    if (c.page_size > 1) {      // positions are below 2^31: with 2^(log - 1) < page_size <= 2^log the rounded-up factor errs by less than one unit
+        int log = 1;
+        while (1LL << log < c.page_size) ++log;
+        n.magic = (uint32_t)(((1ull << (31 + log)) + c.page_size - 1) / c.page_size);
+        n.shift = log - 1;
+    }
+    const dim3 grid((unsigned)((c.heads + heads - 1) / heads), (unsigned)std::min(n.s_tiles, 65535), (unsigned)std::min(t.B, 65535)), block(256);
     if (!write) {
         hipLaunchKernelGGL((kv_read_kernel<T, L>), grid, block, 0, st, rows, c, t, n);
     } else if (vec) {
