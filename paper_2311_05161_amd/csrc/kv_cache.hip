@@ -59,21 +59,33 @@ __device__ __forceinline__ RowScale row_scale(float lo_neg, float hi)
     return r;
 }
 
-// Eight values -> their packed word
+// Eight values -> their packed word.  Every instruction counts here (17 for each value take as long as the memory does): the rounding
+// addition carries the zero-point, made even (which leaves ties to even codes where they are), the packed codes lose what that was
+// too much, and the sign of the two special levels comes in for all eight at once.
 __device__ __forceinline__ uint32_t encode8(const float (&x)[8], const RowScale &r)
 {
-    const float q1 = 0.25f * r.step, q3 = 0.75f * r.step;
+    const float q1 = 0.25f * r.step, q3 = 0.75f * r.step, lo = -r.zero, hi = 13.0f - r.zero;
+    const uint32_t odd = (uint32_t)r.zero & 1u;
+    const float magic = KV_MAGIC + (r.zero + (float)odd);
     uint32_t c[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float u = __builtin_fmaf(x[j], r.inv, x[j] * r.inv_lo);
-        const float k = fminf(fmaxf(u, -r.zero), 13.0f - r.zero);    // (the ends are integers: clamping first changes nothing)
-        const uint32_t code = __float_as_uint((k + KV_MAGIC) + r.zero);
-        const uint32_t half = 14u + (__float_as_uint(x[j]) >> 31);
+        const uint32_t code = __float_as_uint(__builtin_amdgcn_fmed3f(u, lo, hi) + magic);   // (the ends are integers: clamping first changes nothing)
         const float ax = fabsf(x[j]);
-        c[j] = ((ax > q1) & (ax <= q3)) ? half : code;
+        c[j] = ((ax > q1) & (ax <= q3)) ? 14u + odd : code;
     }
-    return recode8(pack4_low_bytes(c[0], c[1], c[2], c[3]), pack4_low_bytes(c[4], c[5], c[6], c[7]), 0x01010101u);
+    const uint32_t a = pack4_low_bytes(c[0], c[1], c[2], c[3]), b = pack4_low_bytes(c[4], c[5], c[6], c[7]);
+    const uint32_t n = (a | (b << 4)) - odd * 0x11111111u;  // (every nibble is at least `odd`)
+    // recode8 with 14 for both special levels: the upper member is the positive one
+    const auto signs = [&](int j) {                         // the sign bits of four values, at bit 0 of their bytes
+        const uint32_t s01 = __builtin_amdgcn_perm(__float_as_uint(x[j + 1]), __float_as_uint(x[j]), 0x0c0c0703u);
+        const uint32_t s23 = __builtin_amdgcn_perm(__float_as_uint(x[j + 3]), __float_as_uint(x[j + 2]), 0x07030c0cu);
+        return ((s01 | s23) >> 7) & 0x01010101u;
+    };
+    const uint32_t minus = signs(0) | (signs(4) << 4);
+    const uint32_t m = (n >> 3) & (n >> 2) & (n >> 1) & 0x11111111u;
+    return ((n >> 1) & 0x77777777u) | (((n & 0x11111111u) ^ (m & ~minus)) << 3);
 }
 
 __device__ __forceinline__ int64_t kv_place(const KvTokens &t, const KvView &c, const KvTiles &n, int b, int head, int token)
@@ -88,11 +100,16 @@ template <typename T, int L, bool VEC>
 __global__ __launch_bounds__(256) void kv_write_kernel(KvRows in, KvView c, KvTokens t, KvTiles n)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & (L - 1), g = (threadIdx.x & 63) / L, words = c.D / 8;
-    const int heads = 64 / L >> n.tokens_log, head = (blockIdx.x * 4 + wave) * heads + (g >> n.tokens_log);
+    const int heads = 64 / L >> n.tokens_log, head = (blockIdx.x * 4 + wave) * heads + (g >> n.tokens_log), sg = g & ((1 << n.tokens_log) - 1);
+    // (VEC: a tile's rows are less than 2^31 bytes apart)
+    int64_t off[2];
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+        off[kv] = VEC ? (int64_t)((int)__umul24(sg, (int)in.ld_s[kv]) + (int)__umul24(head, (int)in.ld_h[kv]) + lane * 8) : sg * in.ld_s[kv] + head * in.ld_h[kv] + lane * 8;
     for (int b = blockIdx.z; b < t.B; b += gridDim.z) {
         const KvLength len = kv_length(t, c, b);
         for (int tile = blockIdx.y; tile < n.s_tiles; tile += gridDim.y) {
-            const int s = (tile << n.tokens_log) + (g & ((1 << n.tokens_log) - 1));
+            const int s = (tile << n.tokens_log) + sg;
             const bool there = s < len.count && head < c.heads;
             float x[2][8];
 #pragma unroll
@@ -100,7 +117,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvRows in, KvView c, KvTo
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[kv][j] = 0.0f;
                 if (there && lane < words) {
-                    const T *p = (const T *)in.x[kv] + b * in.ld_b[kv] + s * in.ld_s[kv] + head * in.ld_h[kv] + lane * 8;
+                    const T *p = (const T *)in.x[kv] + (b * in.ld_b[kv] + ((int64_t)tile << n.tokens_log) * in.ld_s[kv]) + off[kv];
                     if (VEC) {
                         widen8(load_raw8<T>(p), x[kv]);
                     } else {
@@ -114,9 +131,9 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvRows in, KvView c, KvTo
             for (int kv = 0; kv < 2; ++kv) {
                 float lo = 0.0f, hi = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    lo = fmaxf(lo, -x[kv][j]);
-                    hi = fmaxf(hi, x[kv][j]);
+                for (int j = 0; j < 8; j += 2) {
+                    lo = fmaxf(fmaxf(lo, -x[kv][j]), -x[kv][j + 1]);
+                    hi = fmaxf(fmaxf(hi, x[kv][j]), x[kv][j + 1]);
                 }
                 const RowScale r = row_scale(group_max<L>(lo), group_max<L>(hi));
                 if (row >= 0 && lane < words) {
@@ -201,7 +218,10 @@ static int launch_kv(bool write, const KvRows &rows, const KvView &c, const KvTo
         n.magic = (uint32_t)(((1ull << (31 + log)) + c.page_size - 1) / c.page_size);
         n.shift = log - 1;
     }
-    const dim3 grid((unsigned)((c.heads + heads - 1) / heads), (unsigned)std::min(n.s_tiles, 65535), (unsigned)std::min(t.B, 65535)), block(256);
+    // much work: four tiles to a wave, which pays for its addresses once
+    const int64_t h_tiles = (c.heads + heads - 1) / heads;
+    const int per = h_tiles * n.s_tiles * t.B >= 16384 ? 4 : 1;
+    const dim3 grid((unsigned)h_tiles, (unsigned)std::min((n.s_tiles + per - 1) / per, 65535), (unsigned)std::min(t.B, 65535)), block(256);
     if (!write) {
         hipLaunchKernelGGL((kv_read_kernel<T, L>), grid, block, 0, st, rows, c, t, n);
     } else if (vec) {
@@ -217,7 +237,8 @@ static int launch_kv_t(bool write, const KvRows &rows, const KvView &c, const Kv
 {
     bool vec = true;
     for (int kv = 0; kv < 2; ++kv)
-        vec = vec && (uintptr_t)rows.x[kv] % 16 == 0 && (rows.ld_b[kv] | rows.ld_s[kv] | rows.ld_h[kv]) * (int64_t)sizeof(T) % 16 == 0;
+        vec = vec && (uintptr_t)rows.x[kv] % 16 == 0 && (rows.ld_b[kv] | rows.ld_s[kv] | rows.ld_h[kv]) * (int64_t)sizeof(T) % 16 == 0 &&
+              (uint64_t)rows.ld_s[kv] < 1u << 24 && (uint64_t)rows.ld_h[kv] < 1u << 24 && 8 * rows.ld_s[kv] + (c.heads + 32) * rows.ld_h[kv] < 1LL << 29;
     const int words = c.D / 8;
     if (words <= 8) return launch_kv<T, 8>(write, rows, c, t, vec, st);
     if (words <= 16) return launch_kv<T, 16>(write, rows, c, t, vec, st);
