@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvRows in, KvView c, KvTo
                     lo = fmaxf(fmaxf(lo, -x[kv][j]), -x[kv][j + 1]);
                     hi = fmaxf(fmaxf(hi, x[kv][j]), x[kv][j + 1]);
                 }
-                const RowScale r = row_scale(group_max<L>(lo), group_max<L>(hi));
+                const RowScale r = row_scale(group_max_positive<L>(lo), group_max_positive<L>(hi));
                 if (row >= 0 && lane < words) {
                     reinterpret_cast<uint32_t *>(c.packed[kv])[row * words + lane] = encode8(x[kv], r);
                     if (lane == 0) c.words[kv][row] = __float_as_int(r.step) | (int)r.zero;

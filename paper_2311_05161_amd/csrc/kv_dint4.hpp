@@ -59,16 +59,18 @@ __device__ __forceinline__ void kv_decode8(uint32_t p, const DecodeLut &t, float
 __device__ __forceinline__ float kv_step(int32_t word) { return __int_as_float(word & -16); }
 
 // reductions over groups of L lanes (a power of two); all 64 lanes active
+// (numbers that are not negative are ordered as their bits are, and the integer maximum takes the other lane's value as it comes)
 template <int L>
-__device__ __forceinline__ float group_max(float v)
+__device__ __forceinline__ float group_max_positive(float f)
 {
-    if (L > 1) v = fmaxf(v, dpp_f32<DPP_QUAD_XOR1>(v));
-    if (L > 2) v = fmaxf(v, dpp_f32<DPP_QUAD_XOR2>(v));
-    if (L > 4) v = fmaxf(v, dpp_f32<DPP_ROW_HALF_MIRROR>(v));
-    if (L > 8) v = fmaxf(v, dpp_f32<DPP_ROW_MIRROR>(v));
-    if (L > 16) v = fmaxf(v, __shfl_xor(v, 16));
-    if (L > 32) v = fmaxf(v, __shfl_xor(v, 32));
-    return v;
+    uint32_t v = __float_as_uint(f) & 0x7fffffffu;          // (-0 is 0)
+    if (L > 1) v = max(v, (uint32_t)dpp_i32<DPP_QUAD_XOR1>((int)v));
+    if (L > 2) v = max(v, (uint32_t)dpp_i32<DPP_QUAD_XOR2>((int)v));
+    if (L > 4) v = max(v, (uint32_t)dpp_i32<DPP_ROW_HALF_MIRROR>((int)v));
+    if (L > 8) v = max(v, (uint32_t)dpp_i32<DPP_ROW_MIRROR>((int)v));
+    if (L > 16) v = max(v, (uint32_t)__shfl_xor((int)v, 16));
+    if (L > 32) v = max(v, (uint32_t)__shfl_xor((int)v, 32));
+    return __uint_as_float(v);
 }
 template <int L>
 __device__ __forceinline__ float group_sum(float v)
