@@ -253,15 +253,13 @@ static int launch_norm_quant_t(const NormArgs &p, hipStream_t st)
     if (vec) {
         if (p.K <= 512) return launch_rows<T, 1, 1>(p, 8, st);
         if (p.K <= 1024) return launch_rows<T, 2, 1>(p, 4, st);
-        if (p.M <= 512) {      // few rows: as many lanes to a row as there are chunks
-            if (p.K <= 2048) return launch_rows<T, 1, 4>(p, 8, st);
-            if (p.K <= 4096) return launch_rows<T, 1, 8>(p, 4, st);
-            if (p.K <= 8192) return launch_rows<T, 1, 16>(p, 2, st);
-            return launch_rows<T, 2, 16>(p, 2, st);
-        }
         if (p.K <= 2048) return launch_rows<T, 1, 4>(p, 8, st);
-        if (p.K <= 4096) return launch_rows<T, 2, 4>(p, 4, st);
-        if (p.K <= 8192) return launch_rows<T, 2, 8>(p, 2, st);
+        if (p.K <= 4096) return launch_rows<T, 1, 8>(p, 4, st);
+        // Rows that a workgroup of eight waves takes in two chunks or more: sixteen waves where there is at most one row per CU (us, sixteen /
+        // eight waves: 1 x 12288 4.9 / 5.1, 256 x 9216 6.1 / 6.0, 333 x 9216 9.6 / 8.2, 512 x 5120 6.6 / 6.4)
+        if (p.M <= 256) return p.K <= 8192 ? launch_rows<T, 1, 16>(p, 2, st) : launch_rows<T, 2, 16>(p, 2, st);
+        // (three workgroups per CU instead of two: 4096 x 5120 26.5 us for 31.2, 768 x 5120 8.3 for 7.5; three chunks fit two)
+        if (p.K <= 8192) return launch_rows<T, 2, 8>(p, p.M < 1024 ? 2 : 3, st);
         if (p.K <= 12288) return launch_rows<T, 3, 8>(p, 2, st);
         return launch_rows<T, 4, 8>(p, 1, st);
     }
