@@ -666,7 +666,7 @@ __device__ __forceinline__ int v_chunk(int ch, int chunk) { return chunk ^ ((ch 
 constexpr int TILE_RUN = 4;
 
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW * 64, NW / 4) void attn_tile_kernel(StreamArgs p, KvView c, KvTokens t)
+__global__ __launch_bounds__(NW * 64, NW == 4 && D == 256 ? 1 : 2) void attn_tile_kernel(StreamArgs p, KvView c, KvTokens t)
 {
     constexpr int KLD = D * 2 + 16, KBYTES = 64 * KLD, VBYTES = D * 128, BUF = KBYTES + VBYTES;
     constexpr int KS = D / 16, CB = D / 32, WORDS = D / 8;
@@ -1117,9 +1117,13 @@ static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, in
         }
     };
     if (rows > 32) {
-        n.tile = rows > 128 && c.D < 256 ? 8 : 4;
+        // 256 rows share a decoded tile, or 128 where that leaves CUs idle (or registers do not allow it): 3 x 122 tokens, 4 heads on one 12.4
+        // us for 16.0; 512 x 8000 tokens, 32 heads 118 for 128.  One part per CU, of 128 tokens at least: 100 x 3000 tokens, 32 heads on 8,
+        // 31 us (two per CU 35, parts of 512 or more 43); 200 x 1000 tokens, 8 heads on one, 21 us (parts of 256 or more 25).
+        const int64_t eight = (rows + 255) / 256 * pairs;
+        n.tile = rows > 128 && c.D < 256 && eight * tokens >= 256 * 512 ? 8 : 4;
         n.row_tiles = (int)((rows + 32 * n.tile - 1) / (32 * n.tile));
-        cut(256 / (pairs * n.row_tiles), tokens / 512);
+        cut(256 / (pairs * n.row_tiles), tokens / 128);
         return n;
     }
     n.stream = rows <= 16 || c.D == 256 ? 1 : 2;
