@@ -95,8 +95,8 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs p, KvView c, Kv
 // upper bit added) and half a permute that spreads bytes to halves.  For Keys 16 z + 8 comes off each score with the sum of q; for
 // Values it is taken off before the product (one packed subtraction for two): a token with nearly all of the weight would otherwise
 // leave 2^-20 of 16 z + 8 in channels that are zero.  Queries enter as fp16 as they are (bf16: times a power of two per row, so that nothing is lost); the softmax's weights
-// enter as fp16 numbers p step 2^(12 - E), E the exponent of the largest step so far: their rounding to 11 bits is the only one on
-// the way, 2^24 below the largest p step they still have all of them, and 2^35 below it they end.
+// enter as fp16 numbers p step 2^(13 - E), E the exponent of the largest step so far: their rounding to 11 bits is the only one on
+// the way, 2^25 below the largest p step they still have all of them, and 2^36 below it they end.
 //
 // A wave takes 64 tokens at a time, alone: scores as (16 tokens) x (16 rows) tiles leave in each lane four tokens of one
 // row, which is what the product with the Values (tokens as the inner dimension, 16 channels x 16 rows out) wants as its
@@ -117,9 +117,11 @@ struct StreamArgs {
 constexpr float KV_NONE = -1e30f;      // the maximum of no scores
 constexpr float KV_MASKED = -INFINITY; // (times a row's factor, which is not zero)
 constexpr float KV_LEAST = 1.1754943508222875e-38f;
-// The running maximum M moves when a score passes it by 2^2, and then to 2^2 above the new one: scores have to grow by 2^4 before the next
-// move, which 32 rows over some 30 tiles do a few times (with 2^2 alone, in most of the tiles: 139 us for 118).
-constexpr float KV_SLACK = 2.0f, KV_AHEAD = 2.0f;
+// The running maximum M moves when a score passes it by KV_SLACK, and then to KV_AHEAD above the new one: scores have to grow by 2^3.5
+// before the next move, which 32 rows over some 30 tiles do a few times (with a slack of 2^2 alone, in most of the tiles: 139 us for
+// 136).  p step 2^(13 - E) stays below 2^1.99 2 2^13 < 65504.
+constexpr float KV_SLACK = 1.99f, KV_AHEAD = 1.5f;
+constexpr int KV_UNIT = 13;
 
 __device__ __forceinline__ uint32_t kv_lut_hi(int32_t word) { return ((uint32_t)word << 28) | 0x00C8A888u; }
 constexpr uint32_t KV_LUT_LO = 0x68482808u;
@@ -490,7 +492,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D <= 128 && RP <= 8 ? 3 : 2) vo
                 for (int j = 0; j < NJ; ++j) acc[x][j] *= keep;
             }
         }
-        const float unit = __builtin_ldexpf(1.0f, 12 - E);
+        const float unit = __builtin_ldexpf(1.0f, KV_UNIT - E);
         uint32_t w2[RT][NB][2];                         // weights, two to a word
 #pragma unroll
         for (int x = 0; x < RT; ++x)
@@ -585,7 +587,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D <= 128 && RP <= 8 ? 3 : 2) vo
                 ml[(wave * ROWS + r) * 2] = M[x];
                 ml[(wave * ROWS + r) * 2 + 1] = l[x];
             }
-            const int power = E + 8;                         // 2^24 for the operands, 1/16 for the unit, 2^(E - 12) for the weights
+            const int power = E + 20 - KV_UNIT;             // 2^24 for the operands, 1/16 for the unit, 2^(E - 13) for the weights
             float *dst = os + (wave * ROWS + r) * LD;
 #pragma unroll
             for (int j = 0; j < NJ; ++j)
@@ -663,17 +665,112 @@ __device__ __forceinline__ v4u kv_halves(uint32_t p, int32_t word)
 // eight channels eight apart (the decoder's writes) meet in a bank
 __device__ __forceinline__ int v_chunk(int ch, int chunk) { return chunk ^ ((ch ^ (ch >> 3)) & 7); }
 
+// A tile's rows in the form that the products read, KBYTES of Keys [token][channel] and VBYTES of Values [channel][token chunk], as fp16.
+template <int D> struct TileImage {
+    static constexpr int KLD = D * 2 + 16, KBYTES = 64 * KLD, VBYTES = D * 128, BYTES = KBYTES + VBYTES;
+};
+
+// NW waves' decoding of a tile: half of them Keys, half Values.  A wave has whole blocks of 16 tokens, so a row's address is a scalar
+// and a lane's constant.
+template <int D, int NW> struct TileDecoder {
+    static constexpr int WORDS = D / 8, KLD = TileImage<D>::KLD, KBYTES = TileImage<D>::KBYTES;
+    static constexpr int PW = D == 96 ? 16 : WORDS, TPL = 64 / PW; // lanes to a row, rows to a wave's load
+    static constexpr int DW = NW / 2, BLOCKS = 4 / DW;             // waves that decode Keys (as many decode Values), blocks of 16 tokens for each
+    static constexpr int KT = 16 / TPL, VT = TPL >= 4 ? 1 : 4 / TPL;   // words per lane and block: of Keys; of four tokens' Values
+    static constexpr int RAW = BLOCKS * (KT > 4 * VT ? KT : 4 * VT);
+    bool keys, decodes;
+    int dwave, sub, word;
+    uint32_t raw[RAW];                                             // as they come from memory, with their words
+    int32_t rw[RAW];
+
+    __device__ __forceinline__ TileDecoder(int wave, int lane)
+    {
+        keys = wave < DW;
+        dwave = keys ? wave : wave - DW;
+        sub = lane / PW;
+        word = min(lane - sub * PW, WORDS - 1);
+        decodes = (PW == WORDS || lane - sub * PW < WORDS) && (keys || sub < 4);
+    }
+    __device__ __forceinline__ void load(const TileRows &rows, const KvView &c)
+    {
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n) {
+            const uint32_t at = pick4(rows.row[0], rows.row[1], rows.row[2], rows.row[3], dwave + DW * n);
+            if (keys) {
+                const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[0]) + (uint64_t)at * WORDS;
+                const int32_t *zw = c.words[0] + at;
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    raw[n * KT + k] = src[(uint32_t)(sub * WORDS + word) + k * TPL * WORDS];
+                    rw[n * KT + k] = zw[(uint32_t)sub + k * TPL];
+                }
+            } else {
+                const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[1]) + (uint64_t)at * WORDS;
+                const int32_t *zw = c.words[1] + at;
+#pragma unroll
+                for (int k = 0; k < VT; ++k) {
+                    const uint32_t quad = k * TPL + (TPL > 4 ? sub & 3 : sub);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) raw[4 * (n * VT + k) + r] = src[4 * quad * WORDS + word + r * WORDS];
+                    const v4i z = *reinterpret_cast<const v4i *>(zw + 4 * quad);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) rw[4 * (n * VT + k) + r] = z[r];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void decode(uint8_t *buf) const
+    {
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n) {
+            const int block = dwave + DW * n;
+            if (keys) {
+#pragma unroll
+                for (int k = 0; k < KT; ++k) {
+                    const v4u o = kv_halves(raw[n * KT + k], rw[n * KT + k]);
+                    if (decodes) *reinterpret_cast<v4u *>(buf + (16 * block + sub) * KLD + word * 16 + k * TPL * KLD) = o;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < VT; ++k) {
+                    const int quad = k * TPL + sub, chunk = 2 * block + (quad & 1), off = 8 * (quad >> 1 & 1);
+                    uint32_t lo4[4], hi4[4], lut[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t w = raw[4 * (n * VT + k) + r];
+                        lut[r] = kv_lut_hi(rw[4 * (n * VT + k) + r]);
+                        lo4[r] = kv_bytes(w, lut[r]);
+                        hi4[r] = kv_bytes(w >> 4, lut[r]);
+                    }
+                    v2h zero[2];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        zero[r] = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(lut[2 * r + 1], lut[2 * r], 0x0c070c03u) | 0x00080008u);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t sel = 0x0c040c00u + (uint32_t)(j & 3) * 0x00010001u;
+                        v2u o;
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const uint32_t two = j < 4 ? __builtin_amdgcn_perm(lo4[2 * r + 1], lo4[2 * r], sel) : __builtin_amdgcn_perm(hi4[2 * r + 1], hi4[2 * r], sel);
+                            o[r] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, two) - zero[r]);
+                        }
+                        const int ch = 8 * word + j;
+                        if (decodes) *reinterpret_cast<v2u *>(buf + KBYTES + ch * 128 + v_chunk(ch, chunk) * 16 + off) = o;
+                    }
+                }
+            }
+        }
+    }
+};
+
 constexpr int TILE_RUN = 4;
 
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 4 && D == 256 ? 1 : 2) void attn_tile_kernel(StreamArgs p, KvView c, KvTokens t)
 {
-    constexpr int KLD = D * 2 + 16, KBYTES = 64 * KLD, VBYTES = D * 128, BUF = KBYTES + VBYTES;
-    constexpr int KS = D / 16, CB = D / 32, WORDS = D / 8;
-    constexpr int PW = D == 96 ? 16 : WORDS, TPL = 64 / PW; // lanes to a row, rows to a wave's load
-    constexpr int DW = NW / 2, BLOCKS = 4 / DW;             // waves that decode Keys (as many decode Values), blocks of 16 tokens for each
-    constexpr int KT = 16 / TPL, VT = TPL >= 4 ? 1 : 4 / TPL;   // words per lane and block: of Keys; of four tokens' Values
-    constexpr int RAW = BLOCKS * (KT > 4 * VT ? KT : 4 * VT);
+    constexpr int KLD = TileImage<D>::KLD, KBYTES = TileImage<D>::KBYTES, BUF = TileImage<D>::BYTES;
+    constexpr int KS = D / 16, CB = D / 32;
     extern __shared__ uint8_t tile_lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, kg = lane >> 5;
@@ -682,7 +779,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D == 256 ? 1 : 2) void attn_til
     id /= p.splits;
     // longest tiles first, and the row tiles of a (sequence, head) in runs of TILE_RUN: workgroups go to an XCD's four shader engines in
     // turn whether these are busy or not, so a period of 2 or 4 in what they have to do would leave engines idle (two sequences of
-    // 3000 and 743 tokens, the short one's empty workgroups every second place: 226 us; in runs 160)
+    // 3000 and 743 tokens, the short one's empty workgroups every second place: 226 us, 129 in runs)
     const int in_run = id / c.heads, h = id - in_run * c.heads, b = blockIdx.y;
     const int rt = p.row_tiles - 1 - ((int)blockIdx.z * min(TILE_RUN, p.row_tiles) + in_run);
     if (rt < 0) return;
@@ -735,82 +832,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D == 256 ? 1 : 2) void attn_til
 
         // ---- the tiles' rows
         TileRows rows(c, t, b, h, t0, p.page_jump, p.page_rest);
-        // What this thread decodes, as it comes from memory: a wave has whole blocks of 16 tokens, so a row's address is a scalar and a
-        // lane's constant.
-        const bool keys = wave < DW;
-        const int dwave = keys ? wave : wave - DW, sub = lane / PW, word = min(lane - sub * PW, WORDS - 1);
-        const bool decodes = (PW == WORDS || lane - sub * PW < WORDS) && (keys || sub < 4);
-        uint32_t raw[RAW];
-        int32_t rw[RAW];
-        auto load_raw = [&]() {
-#pragma unroll
-            for (int n = 0; n < BLOCKS; ++n) {
-                const uint32_t at = pick4(rows.row[0], rows.row[1], rows.row[2], rows.row[3], dwave + DW * n);
-                if (keys) {
-                    const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[0]) + (uint64_t)at * WORDS;
-                    const int32_t *zw = c.words[0] + at;
-#pragma unroll
-                    for (int k = 0; k < KT; ++k) {
-                        raw[n * KT + k] = src[(uint32_t)(sub * WORDS + word) + k * TPL * WORDS];
-                        rw[n * KT + k] = zw[(uint32_t)sub + k * TPL];
-                    }
-                } else {
-                    const uint32_t *src = reinterpret_cast<const uint32_t *>(c.packed[1]) + (uint64_t)at * WORDS;
-                    const int32_t *zw = c.words[1] + at;
-#pragma unroll
-                    for (int k = 0; k < VT; ++k) {
-                        const uint32_t quad = k * TPL + (TPL > 4 ? sub & 3 : sub);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) raw[4 * (n * VT + k) + r] = src[4 * quad * WORDS + word + r * WORDS];
-                        const v4i z = *reinterpret_cast<const v4i *>(zw + 4 * quad);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) rw[4 * (n * VT + k) + r] = z[r];
-                    }
-                }
-            }
-        };
-        auto decode_raw = [&](uint8_t *buf) {
-#pragma unroll
-            for (int n = 0; n < BLOCKS; ++n) {
-                const int block = dwave + DW * n;
-                if (keys) {
-#pragma unroll
-                    for (int k = 0; k < KT; ++k) {
-                        const v4u o = kv_halves(raw[n * KT + k], rw[n * KT + k]);
-                        if (decodes) *reinterpret_cast<v4u *>(buf + (16 * block + sub) * KLD + word * 16 + k * TPL * KLD) = o;
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < VT; ++k) {
-                        const int quad = k * TPL + sub, chunk = 2 * block + (quad & 1), off = 8 * (quad >> 1 & 1);
-                        uint32_t lo4[4], hi4[4], lut[4];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const uint32_t w = raw[4 * (n * VT + k) + r];
-                            lut[r] = kv_lut_hi(rw[4 * (n * VT + k) + r]);
-                            lo4[r] = kv_bytes(w, lut[r]);
-                            hi4[r] = kv_bytes(w >> 4, lut[r]);
-                        }
-                        v2h zero[2];
-#pragma unroll
-                        for (int r = 0; r < 2; ++r)
-                            zero[r] = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(lut[2 * r + 1], lut[2 * r], 0x0c070c03u) | 0x00080008u);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const uint32_t sel = 0x0c040c00u + (uint32_t)(j & 3) * 0x00010001u;
-                            v2u o;
-#pragma unroll
-                            for (int r = 0; r < 2; ++r) {
-                                const uint32_t two = j < 4 ? __builtin_amdgcn_perm(lo4[2 * r + 1], lo4[2 * r], sel) : __builtin_amdgcn_perm(hi4[2 * r + 1], hi4[2 * r], sel);
-                                o[r] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, two) - zero[r]);
-                            }
-                            const int ch = 8 * word + j;
-                            if (decodes) *reinterpret_cast<v2u *>(buf + KBYTES + ch * 128 + v_chunk(ch, chunk) * 16 + off) = o;
-                        }
-                    }
-                }
-            }
-        };
+        TileDecoder<D, NW> dec(wave, lane);
         // the words of Keys and Values for the softmax: lane i & 15's token, in the first and the second 32
         int32_t stw[2][2];
         auto load_steps = [&](uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
@@ -827,12 +849,12 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D == 256 ? 1 : 2) void attn_til
 #pragma unroll
         for (int s = 0; s < 4; ++s) v_off[s] = col * 128 + v_chunk(col, 2 * s + kg) * 16;
         rows.next();
-        load_raw();
+        dec.load(rows, c);
         load_steps(rows.row[0], rows.row[1], rows.row[2], rows.row[3]);
         uint32_t ok_now = rows.ok;
-        decode_raw(tile_lds);
+        dec.decode(tile_lds);
         rows.next();
-        if (t0 + 64 < t1) load_raw();
+        if (t0 + 64 < t1) dec.load(rows, c);
         int buf = 0;
         for (int tok = t0; tok < t1; tok += 64) {
             // One barrier a tile: behind it this tile is in LDS and the other buffer is free.  The next tile's Values are decoded in front of
@@ -858,9 +880,9 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D == 256 ? 1 : 2) void attn_til
                 ok_now = rows.ok;
             }
             rows.next();
-            if (!keys) {
-                if (more) decode_raw(other);
-                if (more2) load_raw();
+            if (!dec.keys) {
+                if (more) dec.decode(other);
+                if (more2) dec.load(rows, c);
             }
             if (tok < lim_hi) {
                 v16f y[2];
@@ -918,7 +940,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D == 256 ? 1 : 2) void attn_til
 #pragma unroll
                         for (int i = 0; i < 16; ++i) acc[k][i] *= keep;
                 }
-                const float unit = __builtin_ldexpf(1.0f, 12 - E);
+                const float unit = __builtin_ldexpf(1.0f, KV_UNIT - E);
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb) {
                     const float svn = sv[tb] * unit;
@@ -942,16 +964,16 @@ __global__ __launch_bounds__(NW * 64, NW == 4 && D == 256 ? 1 : 2) void attn_til
                         }
                 }
             }
-            if (keys) {
-                if (more) decode_raw(other);
-                if (more2) load_raw();
+            if (dec.keys) {
+                if (more) dec.decode(other);
+                if (more2) dec.load(rows, c);
             }
         }
     }
 
     if (my_row >= p.rows) return;
     l += __shfl_xor(l, 32);                                 // (lanes 32 apart have the same row)
-    const int s = my_row / group, power = E + 8;            // 2^24 for the operands, 1/16 for the unit, 2^(E - 12) for the weights
+    const int s = my_row / group, power = E + 20 - KV_UNIT; // 2^24 for the operands, 1/16 for the unit, 2^(E - 13) for the weights
     if (s >= len.count) l = 0.0f;
     if (p.splits == 1) {
         T *out = (T *)p.a.out + (((int64_t)b * t.S + s) * p.a.Hq + h * group + (my_row - s * group)) * D;

@@ -226,3 +226,20 @@ def test_refusals():
         run(q[..., :32], cache, [5], None, table)
     with pytest.raises(KeyError):
         run(q.double(), cache, [5], None, table)
+
+
+@pytest.mark.parametrize("D,dtype,P", [(128, "f16", 16), (96, "bf16", 64), (64, "f16", 48)])
+def test_many_rows_over_many_tokens(D, dtype, P):
+    """Several tiles of 256 rows over many tokens: unequal lengths, pages that are not there, garbage behind."""
+    B, S, H, G, T = 2, 1300, 4, 1, 2800
+    start, count = [T - S, 700], [S, 333]
+    q, cache, table = setup(B, S, G * H, H, D, T, P, dtype)
+    table[0, 700 // P], table[1, 3] = -1, 1 << 20
+    ref = check(q, cache, start, count, table, max_len=T)
+    assert (ref[1, 333:] == 0).all()
+    bad = [t.clone() for t in cache]
+    for p in range(start[1] + count[1], table.shape[1] * P):
+        page = int(table[1, p // P])
+        bad[1][page, :, p % P], bad[3][page, :, p % P], bad[2][page, :, p % P] = 0x7FC00003, 0x7F800000, 0xFF
+    assert torch.equal(run(q, bad, start, count, table, max_len=T).view(torch.int16), ref.view(torch.int16))
+    check(q, cache, start, count, table, max_len=2000)
