@@ -3,6 +3,12 @@
 //     o[b, i, h] = sum_t p_t v_t,   p = softmax_t(scale q[b, i, h] . k_t),   t = 0 .. start[b] + i
 //
 // with the h / (Hq / Hkv)-th head of the cache.  A query that is not there (i >= count[b]) gives zeros.
+//
+// Three kernels.  Up to 32 query rows per head of the cache (single tokens, with their groups) every byte of the cache is read once and
+// memory bounds it: the streaming kernel, from memory to matrix cores without LDS.  More rows share decoded tiles in LDS, and vector
+// operations (decoding, softmax) beside the matrix instructions bound it: the tile kernel.  What these two do not take (binary32, pages
+// that are not multiples of 16 tokens, other head sizes) goes row by row.  Where there are fewer workgroups than CUs the tokens
+// are cut into parts, each with its maximum, sum and output, joined by a second launch (it would need cleared counters in one).
 #include <algorithm>
 #include <utility>
 
@@ -25,7 +31,9 @@ template <> __device__ __forceinline__ __half attn_from_f32<__half>(float v) { r
 template <> __device__ __forceinline__ bf16_t attn_from_f32<bf16_t>(float v) { return bf16_t{f32_to_bf16_bits(v)}; }
 
 // Any head size (a multiple of 8, at most 512), page size and alignment: a workgroup per query row, L lanes (8 channels each) per
-// token, 256 / L tokens at a time, each group of lanes with a running maximum, sum and output of its own, joined at the end.
+// token, 256 / L tokens at a time, each group of lanes with a running maximum, sum and output of its own, joined at the end.  A row
+// reads the cache for itself, in binary32 throughout: bfloat16, 8 x 1 of
+// 4096 tokens, 32 heads of 128, pages of 8 tokens 368 us (pages of 64, by the streaming kernel 36); 1 x 1 of 600 30 us (9.3).
 template <typename T, int L>
 __global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs p, KvView c, KvTokens t)
 {
@@ -264,8 +272,17 @@ template <int D> struct StreamShape {
     static constexpr int NJ = HALVES ? 4 : 8 * VW;         // channels per lane
 };
 
+// Waves to a SIMD: as many as the registers of a wave's tile of 64 tokens allow.  One where two would spill (us, spilled / one wave: 32 rows, 8 x
+// 8192 tokens, 8 heads of 128 53 / 42; 16 rows, heads of 256 63 / 50), with workgroups of four waves; three of four waves where that does
+// not (8 rows, 64 x 4096 tokens, 8 heads of 128: three, spilling, 71.4, two 68.4).
+constexpr bool stream_wide(int D, int RP, int RT) { return RT == 2 || (D == 256 && RP >= 8); }
+constexpr int stream_occupancy(int D, int RP, int RT, int NW)
+{
+    return stream_wide(D, RP, RT) ? 1 : NW == 4 && (RP == 4 ? D <= 128 : RP == 8 && D <= 64) ? 3 : 2;
+}
+
 template <typename T, int D, int RP, int RT, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 4 && D <= 128 && RP <= 8 ? 3 : 2) void attn_stream_kernel(StreamArgs p, KvView c, KvTokens t)
+__global__ __launch_bounds__(NW * 64, stream_occupancy(D, RP, RT, NW)) void attn_stream_kernel(StreamArgs p, KvView c, KvTokens t)
 {
     using Shape = StreamShape<D>;
     constexpr int W = Shape::W, VW = Shape::VW, NJ = Shape::NJ;
@@ -1148,12 +1165,15 @@ static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, in
         cut(256 / (pairs * n.row_tiles), tokens / 128);
         return n;
     }
-    n.stream = rows <= 16 || c.D == 256 ? 1 : 2;
+    // 17 .. 32 rows: one workgroup for all of them, where two would read the cache twice for work that fills the chip anyway (us, one / two
+    // workgroups: 32 rows, 8 x 8192 tokens, 8 heads 42 / 52; 24 rows, 32 x 200, 8 heads 13 / 16), not where there is little (8 x 2000 23 / 20;
+    // 2 x 16000, one head 22.4 / 18.2).
+    n.stream = rows > 16 && (pairs > 128 || pairs * tokens >= 256 * 1024) ? 2 : 1;
     n.rp = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
     // Many sequences and heads: workgroups of four waves, three to a CU (as the registers allow), keep more loads in flight than one of
     // eight (32 x 4096 tokens, 40 heads: 164 us for 185); few: eight waves per part, i.e. half as many parts to join (131073
     // tokens, 8 heads: 49 us for 58; 600 tokens, 32 heads: 9.0 for 11.7).
-    n.waves = pairs >= 512 ? 4 : 8;
+    n.waves = pairs >= 512 || stream_wide((int)c.D, n.rp, n.stream) ? 4 : 8;
     n.row_tiles = (int)((rows + 16 * n.stream - 1) / (16 * n.stream));
     const int64_t tile = n.waves * 64;
     // One workgroup to a CU at a time (registers), so as many parts as there are CUs: each is as long as it can be, and the queries, the
@@ -1206,13 +1226,11 @@ static int launch_stream_d(const AttnPlan &n, const StreamArgs &p, const KvView 
         return W4A8_ERR_SHAPE;
     }
     if (n.tile == 4) return launch_tile<T, D, 4>(p, c, t, st);
-    if (n.stream == 2) {
-        if constexpr (D <= 128) return n.waves == 4 ? launch_stream<T, D, 16, 2, 4>(p, c, t, st) : launch_stream<T, D, 16, 2, 8>(p, c, t, st);
-        return W4A8_ERR_SHAPE;
-    }
-    if (n.rp == 4) return n.waves == 4 ? launch_stream<T, D, 4, 1, 4>(p, c, t, st) : launch_stream<T, D, 4, 1, 8>(p, c, t, st);
-    if (n.rp == 8) return n.waves == 4 ? launch_stream<T, D, 8, 1, 4>(p, c, t, st) : launch_stream<T, D, 8, 1, 8>(p, c, t, st);
-    return n.waves == 4 ? launch_stream<T, D, 16, 1, 4>(p, c, t, st) : launch_stream<T, D, 16, 1, 8>(p, c, t, st);
+    if (n.stream == 2) return launch_stream<T, D, 16, 2, 4>(p, c, t, st);
+    if (n.waves == 4) return n.rp == 4 ? launch_stream<T, D, 4, 1, 4>(p, c, t, st) : n.rp == 8 ? launch_stream<T, D, 8, 1, 4>(p, c, t, st) : launch_stream<T, D, 16, 1, 4>(p, c, t, st);
+    if (n.rp == 4) return launch_stream<T, D, 4, 1, 8>(p, c, t, st);
+    if constexpr (D <= 128) return n.rp == 8 ? launch_stream<T, D, 8, 1, 8>(p, c, t, st) : launch_stream<T, D, 16, 1, 8>(p, c, t, st);
+    return W4A8_ERR_SHAPE;      // (wide ones have four waves)
 }
 
 template <typename T>

@@ -243,3 +243,30 @@ def test_many_rows_over_many_tokens(D, dtype, P):
         bad[1][page, :, p % P], bad[3][page, :, p % P], bad[2][page, :, p % P] = 0x7FC00003, 0x7F800000, 0xFF
     assert torch.equal(run(q, bad, start, count, table, max_len=T).view(torch.int16), ref.view(torch.int16))
     check(q, cache, start, count, table, max_len=2000)
+
+
+@pytest.mark.parametrize("S,G,D,dtype,P", [(6, 4, 128, "f16", 16), (4, 8, 128, "bf16", 64), (17, 1, 64, "bf16", 16), (9, 3, 96, "f16", 48), (5, 4, 256, "bf16", 32), (32, 1, 256, "f16", 16)])
+def test_17_to_32_rows_of_many_sequences(S, G, D, dtype, P):
+    """More (sequence, head) pairs than workgroups need to be cut: unequal lengths, pages that are not there, garbage behind."""
+    B, H, T = 14, 10, 300
+    start, count = [(37 * b) % (T - S + 1) for b in range(B)], [b % (S + 1) for b in range(B)]
+    start[0], count[0], start[1], count[1] = T - S, S, 0, 1
+    q, cache, table = setup(B, S, G * H, H, D, T, P, dtype)
+    table[0, 100 // P], table[4, 0] = -1, 1 << 20
+    ref = check(q, cache, start, count, table, max_len=T)
+    for b in range(B):
+        assert (ref[b, count[b]:] == 0).all()
+    bad = [t.clone() for t in cache]
+    for b in (1, 5, 9):
+        for p in range(start[b] + count[b], table.shape[1] * P):
+            page = int(table[b, p // P])
+            bad[1][page, :, p % P], bad[3][page, :, p % P], bad[2][page, :, p % P] = 0x7FC00003, 0x7F800000, 0xFF
+    assert torch.equal(run(q, bad, start, count, table, max_len=T).view(torch.int16), ref.view(torch.int16))
+    check(q, cache, start, count, table, max_len=200)
+
+
+@pytest.mark.parametrize("S,G,D", [(4, 8, 128), (3, 8, 256), (20, 1, 96)])
+def test_17_to_32_rows_of_one_long_sequence(S, G, D):
+    B, H, T, P = 1, 10, 27000, 16
+    q, cache, table = setup(B, S, G * H, H, D, T, P, "bf16")
+    check(q, cache, [T - S], None, table)
