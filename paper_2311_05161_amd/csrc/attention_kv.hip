@@ -1156,13 +1156,20 @@ static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, in
         }
     };
     if (rows > 32) {
-        // 256 rows share a decoded tile, or 128 where that leaves CUs idle (or registers do not allow it): 3 x 122 tokens, 4 heads on one 12.4
-        // us for 16.0; 512 x 8000 tokens, 32 heads 118 for 128.  One part per CU, of 128 tokens at least: 100 x 3000 tokens, 32 heads on 8,
-        // 31 us (two per CU 35, parts of 512 or more 43); 200 x 1000 tokens, 8 heads on one, 21 us (parts of 256 or more 25).
-        const int64_t eight = (rows + 255) / 256 * pairs;
-        n.tile = rows > 128 && c.D < 256 && eight * tokens >= 256 * 512 ? 8 : 4;
+        // 256 rows share a decoded tile, or 128: two smaller workgroups fit a CU, decode twice, and leave less idle where causal rows differ
+        // in length.  `mean` is a row's tokens in the mean, `part` the longest part of a workgroup of 256: many long parts, or rows
+        // nearly equal, take 256 (us, 256 / 128 rows: 512 x 8000 tokens, 32 heads 107 / 146; 4096 x 4096, 32 heads on 8 198 / 224; 2 x 1500
+        // x 1500 73 / 80; 700 x 5000 116 / 132), others 128 (2000 x 2000, 32 heads on 8 90 / 80; 16 x 512 x 512 104 / 94; 1000 x 1000, 64 heads of 64
+        // on 8 43 / 37; 2048 x 2048, 40 heads 86 / 78).  (256 rows at heads of 256 do not fit the registers.)
+        const int64_t mean = tokens - std::min<int64_t>(t.S, tokens) / 2;
+        const int64_t eight = (rows + 255) / 256 * pairs, part = tokens / std::max<int64_t>(1, std::min(256 / eight, mean / 128));
+        n.tile = rows > 128 && c.D < 256 && part >= 1024 && eight * mean >= (4 * mean >= 3 * tokens ? 128 : 176) * part ? 8 : 4;
         n.row_tiles = (int)((rows + 32 * n.tile - 1) / (32 * n.tile));
-        cut(256 / (pairs * n.row_tiles), tokens / 128);
+        // One part per CU, of 128 tokens at least (100 x 3000 tokens, 32 heads on 8 29 us, two per CU 35); two where one would leave a third of the
+        // CUs without any (1500 x 1500, 12 heads of 64 35 us for 48).  With that many rows to join, 128 tokens of the mean row (500 x
+        // 500, 32 heads 23 us for 27).
+        const int64_t wgs = pairs * n.row_tiles, two = n.tile == 4 && c.D < 256 && wgs > 128 ? 2 : 1;
+        cut(wgs > 192 ? 1 : two * 256 / wgs, (wgs > 96 ? mean : tokens) / 128);
         return n;
     }
     // 17 .. 32 rows: one workgroup for all of them, where two would read the cache twice for work that fills the chip anyway (us, one / two

@@ -270,3 +270,25 @@ def test_17_to_32_rows_of_one_long_sequence(S, G, D):
     B, H, T, P = 1, 10, 27000, 16
     q, cache, table = setup(B, S, G * H, H, D, T, P, "bf16")
     check(q, cache, [T - S], None, table)
+
+
+@pytest.mark.parametrize("S,G,D,dtype,P", [(150, 1, 128, "f16", 16), (133, 2, 96, "bf16", 48), (260, 1, 64, "f16", 64)])
+def test_some_hundred_rows_over_long_sequences(S, G, D, dtype, P):
+    """Long parts of long sequences: unequal lengths, pages that are not there, garbage behind."""
+    B, H, T = 2, 8, 17000
+    start, count = [T - S, 9001], [S, S - 21]
+    q, cache, table = setup(B, S, G * H, H, D, T, P, dtype)
+    table[0, 2000 // P], table[1, 3] = -1, 1 << 20
+    ref = check(q, cache, start, count, table, max_len=T)
+    assert (ref[1, S - 21:] == 0).all()
+    bad = [t.clone() for t in cache]
+    for p in range(start[1] + count[1], start[1] + count[1] + 300):
+        page = int(table[1, p // P])
+        bad[1][page, :, p % P], bad[3][page, :, p % P], bad[2][page, :, p % P] = 0x7FC00003, 0x7F800000, 0xFF
+    assert torch.equal(run(q, bad, start, count, table, max_len=T).view(torch.int16), ref.view(torch.int16))
+
+
+def test_whole_prompts_of_many_heads():
+    B, S, H, D, P = 3, 1100, 24, 64, 16
+    q, cache, table = setup(B, S, H, H, D, S, P, "bf16")
+    check(q, cache, [0, 0, 0], [S, 517, 0], table, max_len=S)
