@@ -451,7 +451,7 @@ int kv_cache_read_dint4(const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens
  *   max_len   what start[b] + count[b] is at most: work is divided by it, and tokens from there on are not seen
  *   workspace of attention_kv_dint4_workspace_bytes(...) bytes, 256-byte aligned (NULL where that is 0): joined parts of
  *             sequences that are cut; free for reuse once the call's work on `stream` has finished
- * Scores and softmax are binary32; results do not depend on the order in which workgroups run (another max_len may cut the sequences
+ * Scores and softmax are binary32 (F16 and BF16: the weights are rounded to 11 bits for the product with v); results do not depend on the order in which workgroups run (another max_len may cut the sequences
  * in other places and round otherwise). */
 size_t attention_kv_dint4_workspace_bytes(int dtype, int64_t q_heads, const w4a8_kv_cache *cache, const w4a8_kv_tokens *tokens,
                                           int64_t max_len);

@@ -4,7 +4,7 @@ Argument marshalling only: every step of the layer runs in the HIP kernels.  PyT
 device memory (``tensor.data_ptr()``) and the current HIP stream, nothing else.  There is no CPU
 fallback: if the shared library is missing, loading raises.
 
-The online calls (the layer, its two steps, and both for activations with a token zero-point) are
+The online calls (the layer, its two steps, both for activations with a token zero-point, and the norm, cache and attention around them) are
 marshalled in native code (``csrc/native_calls.cpp``) when they are asked for nothing but fresh outputs; the Python
 form beside it takes preallocated outputs, check outputs, workspaces and tensor subclasses, and every call where the
 extension is not there (it is built for one Python and one torch; ``libw4a8.so`` alone does all the work).

@@ -35,7 +35,7 @@ SOURCES = {
 
 COMMON = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-fast-math",
-    # the compiler must not form packed-fp32 instructions on the test machines
+    # the compiler must not form packed-fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wno-unused-command-line-argument",
 ]

@@ -11,6 +11,10 @@
 //     bits and step 20, so u is either a half-integer or at least 2^-21 from one, and u < 16 is rounded by at most that: rne(u)
 //     is that of the exact quotient.  (binary32 inputs: by this u.)
 //   - the step's half-up at bit 20 looks at the sign of the division's remainder, what hi - lo lost included.
+//
+// Memory bounds both ways, just: 2 x 4096 tokens, 40 heads of 128, fp16: the write takes 56 us for 212 MB (3.8 TB/s; its 17 vector
+// operations per value alone would take about as long), the read 35 us for as many (6.0 TB/s).  A step of 16 tokens, 32 heads: 3.8 and 3.7 us,
+// a launch's latency and the chain length -> page -> row.
 #include <algorithm>
 
 #include "kv_dint4.hpp"

@@ -1,7 +1,8 @@
 // Argument marshalling of the layer's online calls in native code.  A decode step of a small layer runs for
 // 5 to 7 us on the GPU; marshalling it in Python (attribute look-ups, two torch.empty, twenty ctypes conversions)
 // took the host about 11 us per call, so that a loop of eager calls was bound by it: 1 x 4096 x 4096 13.9 us a
-// call with it, 5.9 us with this.
+// call with it, 5.9 us with this.  The calls around the layer (norm 6.9 us here on the host, cache write 4.4, read 6.5) bind their
+// smallest steps the same way.
 //
 // Every function takes the address of the C entry point (the library is loaded by Python) and returns
 //   a tensor or a tuple of tensors   on success,
