@@ -31,13 +31,16 @@ template <> __device__ __forceinline__ __half attn_from_f32<__half>(float v) { r
 template <> __device__ __forceinline__ bf16_t attn_from_f32<bf16_t>(float v) { return bf16_t{f32_to_bf16_bits(v)}; }
 
 // Any head size (a multiple of 8, at most 512), page size and alignment: a workgroup per query row, L lanes (8 channels each) per
-// token, 256 / L tokens at a time, each group of lanes with a running maximum, sum and output of its own, joined at the end.  A row
-// reads the cache for itself, in binary32 throughout: bfloat16, 8 x 1 of
-// 4096 tokens, 32 heads of 128, pages of 8 tokens 368 us (pages of 64, by the streaming kernel 36); 1 x 1 of 600 30 us (9.3).
+// token, 512 / L tokens at a time, each group of lanes with a running maximum, sum and output of its own, joined at the end.  A row
+// reads the cache for itself, in binary32 throughout, and vector operations bound it (some 125 for a token and 16 lanes): bfloat16, 8 x 1
+// of 4096 tokens, 32 heads of 128, pages of 8 tokens 121 us (368 with 256 threads and one token of a group in flight; the streaming kernel on
+// pages of 64: 36); 128 of 1000 281 us, 1 of 600 20.
+constexpr int ROWS_WG = 512;
+
 template <typename T, int L>
-__global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs p, KvView c, KvTokens t)
+__global__ __launch_bounds__(ROWS_WG) void attn_rows_kernel(AttnArgs p, KvView c, KvTokens t)
 {
-    constexpr int GROUPS = 256 / L;
+    constexpr int GROUPS = ROWS_WG / L, U = 4;       // tokens of a group in flight
     __shared__ float part_m[GROUPS], part_l[GROUPS];
     __shared__ float part_o[GROUPS][L * 8 + 1];
     const int h = blockIdx.x % p.Hq;
@@ -53,26 +56,49 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs p, KvView c, Kv
         o[j] = 0.0f;
     }
     float m = -INFINITY, l = 0.0f;
-    for (int t0 = 0; t0 < seen; t0 += GROUPS) {      // (uniform: the groups' sums need all lanes)
-        const int64_t at = t0 + g < seen ? kv_row(t, c, b, h / p.group, t0 + g) : -1;
-        const bool mine = at >= 0 && lane < words;
-        float k[8];
-        const int32_t kw = at >= 0 ? c.words[0][at] : 0, vw = at >= 0 ? c.words[1][at] : 0;
-        kv_decode8(mine ? reinterpret_cast<const uint32_t *>(c.packed[0])[at * words + lane] : 0, make_decode_lut(kw & 15), k);
-        float dot = 0.0f;
+    for (int t0 = 0; t0 < seen; t0 += GROUPS * U) {  // (uniform: the groups' sums need all lanes)
+        int64_t at[U];
+        int32_t kw[U], vw[U];
+        uint32_t kp[U], vp[U];
+        float s[U], top = m;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dot = __builtin_fmaf(q[j], k[j], dot);
-        dot = group_sum<L>(dot);
-        if (at >= 0) {                               // (uniform over the group)
-            const float s = dot * (0.125f * kv_step(kw) * p.scale_log2);
-            const float top = fmaxf(m, s), keep = exp2f(m - top), w = exp2f(s - top);
+        for (int u = 0; u < U; ++u) {                // (all loads before the first use)
+            const int token = t0 + u * GROUPS + g;
+            at[u] = token < seen ? kv_row(t, c, b, h / p.group, token) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool mine = at[u] >= 0 && lane < words;
+            kw[u] = at[u] >= 0 ? c.words[0][at[u]] : 0;
+            vw[u] = at[u] >= 0 ? c.words[1][at[u]] : 0;
+            kp[u] = mine ? reinterpret_cast<const uint32_t *>(c.packed[0])[at[u] * words + lane] : 0;
+            vp[u] = mine ? reinterpret_cast<const uint32_t *>(c.packed[1])[at[u] * words + lane] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float k[8], dot = 0.0f;
+            kv_decode8(kp[u], make_decode_lut(kw[u] & 15), k);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dot = __builtin_fmaf(q[j], k[j], dot);
+            dot = group_sum<L>(dot);
+            s[u] = at[u] >= 0 ? dot * (0.125f * kv_step(kw[u]) * p.scale_log2) : -INFINITY;
+            top = fmaxf(top, s[u]);
+        }
+        if (top > -INFINITY) {                       // (uniform over the group)
+            const float keep = exp2f(m - top);
             m = top;
-            l = l * keep + w;
-            float v[8];
-            kv_decode8(mine ? reinterpret_cast<const uint32_t *>(c.packed[1])[at * words + lane] : 0, make_decode_lut(vw & 15), v);
-            const float wv = w * (0.125f * kv_step(vw));
+            l *= keep;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = __builtin_fmaf(wv, v[j], o[j] * keep);
+            for (int j = 0; j < 8; ++j) o[j] *= keep;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float w = exp2f(s[u] - top), wv = w * (0.125f * kv_step(vw[u]));
+                float v[8];
+                kv_decode8(vp[u], make_decode_lut(vw[u] & 15), v);
+                l += w;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = __builtin_fmaf(wv, v[j], o[j]);
+            }
         }
     }
     if (lane == 0) {
@@ -87,7 +113,7 @@ __global__ __launch_bounds__(256) void attn_rows_kernel(AttnArgs p, KvView c, Kv
     const bool any = top > -INFINITY;
     for (int x = 0; x < GROUPS; ++x) sum += any ? part_l[x] * exp2f(part_m[x] - top) : 0.0f;
     T *out = (T *)p.out + (row * p.Hq + h) * (int64_t)c.D;
-    for (int d = tid; d < c.D; d += 256) {
+    for (int d = tid; d < c.D; d += ROWS_WG) {
         float v = 0.0f;
         for (int x = 0; x < GROUPS; ++x) v += any ? part_o[x][d] * exp2f(part_m[x] - top) : 0.0f;
         out[d] = attn_from_f32<T>(any ? v / sum : 0.0f);
@@ -1109,7 +1135,7 @@ static int launch_attn_t(const AttnArgs &p, const KvView &c, const KvTokens &t, 
 {
     const int64_t blocks = (int64_t)t.B * t.S * p.Hq;
     if (blocks > 0x7fffffffLL) return W4A8_ERR_SHAPE;
-    const dim3 grid((unsigned)blocks), block(256);
+    const dim3 grid((unsigned)blocks), block(ROWS_WG);
     const int words = c.D / 8;
     if (words <= 8) {
         hipLaunchKernelGGL((attn_rows_kernel<T, 8>), grid, block, 0, st, p, c, t);
