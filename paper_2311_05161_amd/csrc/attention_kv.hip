@@ -1203,15 +1203,23 @@ static AttnPlan plan_attention(int dtype, const KvView &c, const KvTokens &t, in
     // 2 x 16000, one head 22.4 / 18.2).
     n.stream = rows > 16 && (pairs > 128 || pairs * tokens >= 256 * 1024) ? 2 : 1;
     n.rp = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
-    // Many sequences and heads: workgroups of four waves, three to a CU (as the registers allow), keep more loads in flight than one of
-    // eight (32 x 4096 tokens, 40 heads: 164 us for 185); few: eight waves per part, i.e. half as many parts to join (131073
-    // tokens, 8 heads: 49 us for 58; 600 tokens, 32 heads: 9.0 for 11.7).
-    n.waves = pairs >= 512 || stream_wide((int)c.D, n.rp, n.stream) ? 4 : 8;
+    // More (sequence, head) pairs than CUs: workgroups of four waves, three to a CU (as the registers allow), keep more loads in flight
+    // than one of eight, and do not run in two rounds where there are a few too many (32 x 4096 tokens, 40 heads: 164 us for 185; 10 x
+    // 4096 57 / 61; 12 x 300 9.5 / 13.3).  Fewer: eight waves per part, i.e. half as many parts to join (8 x 4096, 32 heads 33 us for 39;
+    // 131073 tokens, 8 heads: 49 us for 58; 600 tokens, 32 heads: 9.0 for 11.7).
+    const bool many = pairs > 256;
+    n.waves = many || stream_wide((int)c.D, n.rp, n.stream) ? 4 : 8;
     n.row_tiles = (int)((rows + 16 * n.stream - 1) / (16 * n.stream));
     const int64_t tile = n.waves * 64;
-    // One workgroup to a CU at a time (registers), so as many parts as there are CUs: each is as long as it can be, and the queries, the
-    // waves' join and the parts' join are paid for once.  131073 tokens, 8 heads (32 parts): 50 us, 64 parts 62, 128 parts 79.
-    cut(256 / pairs, (tokens + 2 * tile - 1) / (2 * tile));
+    // One workgroup of eight waves to a CU at a time (registers), so as many parts as there are CUs: each is as long as it can be, and the queries, the
+    // waves' join and the parts' join are paid for once.  131073 tokens, 8 heads (32 parts): 50 us, 64 parts 62, 128 parts 79.  Of four
+    // waves: three to a CU, if the parts stay long (34 x 4096 tokens, 8 heads 48 us, uncut 57; 34 x 2000 29.5 / 31; two queries each of 8 heads
+    // to one, 40 x 2000, 8 heads 39 / 37).
+    if (many) {
+        cut(768 / pairs, tokens / 1280);
+    } else {
+        cut(256 / pairs, (tokens + 2 * tile - 1) / (2 * tile));
+    }
     return n;
 }
 

@@ -292,3 +292,16 @@ def test_whole_prompts_of_many_heads():
     B, S, H, D, P = 3, 1100, 24, 64, 16
     q, cache, table = setup(B, S, H, H, D, S, P, "bf16")
     check(q, cache, [0, 0, 0], [S, 517, 0], table, max_len=S)
+
+
+@pytest.mark.parametrize("T", [300, 2600])
+@pytest.mark.parametrize("S,G,D,dtype,P", [(1, 1, 128, "f16", 16), (1, 8, 64, "bf16", 64), (2, 3, 96, "f16", 48), (3, 5, 128, "bf16", 16), (1, 2, 256, "bf16", 32), (2, 8, 256, "f16", 16)])
+def test_a_few_more_sequences_than_compute_units(S, G, D, dtype, P, T):
+    B, H = 33, 8
+    start, count = [(997 * b) % (T - S + 1) for b in range(B)], [b % (S + 1) for b in range(B)]
+    start[0], count[0], start[1], count[1] = T - S, S, 0, 1
+    q, cache, table = setup(B, S, G * H, H, D, T, P, dtype)
+    table[0, 200 // P], table[4, 0] = -1, 1 << 20
+    ref = check(q, cache, start, count, table, max_len=T)
+    for b in range(B):
+        assert (ref[b, count[b]:] == 0).all()
