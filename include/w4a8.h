@@ -426,7 +426,7 @@ typedef struct {
  * (count == NULL: new_tokens each), at positions start[b], start[b] + 1, ..; position p lies in page
  * table[b * table_ld + p / page_size] at place p % page_size.  The arrays are device memory that no call can check before its
  * launch: a negative or too large start or count is clamped to the table, and a position whose page is not one of the cache's is
- * neither written nor seen.  table_pages * page_size < 2^31. */
+ * neither written nor seen.  table_pages * page_size < 2^31, batch and new_tokens <= 2^30. */
 typedef struct {
     const int32_t *start;   /* [batch]                                 */
     const int32_t *count;   /* [batch] or NULL                         */

@@ -212,9 +212,9 @@ static int kv_shape(const w4a8_kv_cache *c, const w4a8_kv_tokens *t)
     if (!c || !t) return W4A8_ERR_NULL;
     if (c->pages < 0 || c->heads < 1 || c->heads > 65535 || c->page_size < 1 || c->page_size > 0x7fffffffLL) return W4A8_ERR_SHAPE;
     if (c->head_dim < 8 || c->head_dim > 512 || c->head_dim % 8 != 0 || c->pages > 0x7fffffffLL || c->page_ld < 0 || c->head_ld < 0) return W4A8_ERR_SHAPE;
-    if (t->batch < 0 || t->batch > 0x7fffffffLL || t->new_tokens < 0 || t->table_pages < 0 || t->table_ld < t->table_pages) return W4A8_ERR_SHAPE;
-    // (positions are numbered in 32 bits, and the step's tokens are part of them)
-    if (t->table_pages > 0x7fffffffLL / c->page_size || t->new_tokens > 0x7fffffffLL) return W4A8_ERR_SHAPE;
+    if (t->batch < 0 || t->batch > 1LL << 30 || t->new_tokens < 0 || t->table_pages < 0 || t->table_ld < t->table_pages) return W4A8_ERR_SHAPE;
+    // (positions are numbered in 32 bits, and the step's tokens are part of them; loops over these go some tiles past them)
+    if (t->table_pages > 0x7fffffffLL / c->page_size || t->new_tokens > 1LL << 30) return W4A8_ERR_SHAPE;
     return W4A8_OK;
 }
 static bool kv_empty(const w4a8_kv_tokens *t) { return t->batch == 0 || t->new_tokens == 0; }

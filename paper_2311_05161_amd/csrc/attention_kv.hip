@@ -56,15 +56,15 @@ __global__ __launch_bounds__(ROWS_WG) void attn_rows_kernel(AttnArgs p, KvView c
         o[j] = 0.0f;
     }
     float m = -INFINITY, l = 0.0f;
-    for (int t0 = 0; t0 < seen; t0 += GROUPS * U) {  // (uniform: the groups' sums need all lanes)
+    for (uint32_t t0 = 0; t0 < (uint32_t)seen; t0 += GROUPS * U) {   // (uniform: the groups' sums need all lanes; may pass 2^31)
         int64_t at[U];
         int32_t kw[U], vw[U];
         uint32_t kp[U], vp[U];
         float s[U], top = m;
 #pragma unroll
         for (int u = 0; u < U; ++u) {                // (all loads before the first use)
-            const int token = t0 + u * GROUPS + g;
-            at[u] = token < seen ? kv_row(t, c, b, h / p.group, token) : -1;
+            const uint32_t token = t0 + u * GROUPS + g;
+            at[u] = token < (uint32_t)seen ? kv_row(t, c, b, h / p.group, (int)token) : -1;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {

@@ -215,7 +215,7 @@ static int launch_kv(bool write, const KvRows &rows, const KvView &c, const KvTo
     const int groups = 64 / L;
     while (1 << n.tokens_log < groups && 1 << n.tokens_log < t.S) ++n.tokens_log;
     const int tokens = 1 << n.tokens_log, heads = 4 * (groups / tokens);
-    n.s_tiles = (t.S + tokens - 1) / tokens;
+    n.s_tiles = (t.S - 1) / tokens + 1;
     if (c.page_size > 1) {      // positions are below 2^31: with 2^(log - 1) < page_size <= 2^log the rounded-up factor errs by less than one unit
         int log = 1;
         while (1LL << log < c.page_size) ++log;
@@ -225,7 +225,7 @@ static int launch_kv(bool write, const KvRows &rows, const KvView &c, const KvTo
     // much work: four tiles to a wave, which pays for its addresses once
     const int64_t h_tiles = (c.heads + heads - 1) / heads;
     const int per = h_tiles * n.s_tiles * t.B >= 16384 ? 4 : 1;
-    const dim3 grid((unsigned)h_tiles, (unsigned)std::min((n.s_tiles + per - 1) / per, 65535), (unsigned)std::min(t.B, 65535)), block(256);
+    const dim3 grid((unsigned)h_tiles, (unsigned)std::min((n.s_tiles - 1) / per + 1, 65535), (unsigned)std::min(t.B, 65535)), block(256);
     if (!write) {
         hipLaunchKernelGGL((kv_read_kernel<T, L>), grid, block, 0, st, rows, c, t, n);
     } else if (vec) {

@@ -129,3 +129,11 @@ def test_definition_is_the_weights_rule(oracle):
     c = codes.astype(np.int64)
     ref = np.where(c == 14, 1, np.where(c == 15, -1, 2 * (c - zero.astype(np.int64)))) * (step / 2.0)
     np.testing.assert_array_equal(du.values64(packed, words).numpy(), ref)
+
+
+@pytest.mark.parametrize("bad", [dict(new_tokens=(1 << 30) + 1), dict(new_tokens=(1 << 31) - 1), dict(batch=(1 << 30) + 1), dict(batch=(1 << 31) - 1)])
+def test_steps_that_32_bits_do_not_hold(lib, bad):
+    c, t = cache_args(head_dim=512), token_args(**bad)
+    assert lib.kv_cache_write_dint4(P16, LD, P16, LD, b.F16, c, t, Z) == b.ERR_SHAPE
+    assert lib.kv_cache_read_dint4(c, t, P16, P16, b.F16, Z) == b.ERR_SHAPE
+    assert lib.attention_kv_dint4(P16, LD, b.F16, 8, c, t, 1.0, 64, P16, Z, 0, Z) == b.ERR_SHAPE
